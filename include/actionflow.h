@@ -279,6 +279,61 @@ af_status af_op_down_residual(af_weights* w, int32_t layer, const void* act, voi
 af_status af_op_lm_head_argmax(af_weights* w, const void* hidden, int32_t M, const af_segment* segs,
                                int32_t n_seg, float* out_logits, int32_t* out_tokens, void* hip_stream);
 
+/* ------------------------------------------------------------------ 8-bit projections and sampling
+ * Operators next to the single steps above, for programs that keep projection weights in 8 bits or
+ * answer with drawn instead of greedy tokens.  Not steps of the paper's method.  None of them
+ * allocates, waits or keeps anything between calls, so they run on any stream, on several at once, and
+ * under graph capture; tensors are dense and row-major, and every pointer is a device pointer.
+ *
+ * 8-bit form: values are e4m3 (4 exponent bits, 3 mantissa bits, largest finite value 448, no
+ * infinity), times one fp32 scale for each block of 128 columns, of one row (activations) or of 128
+ * rows (weights); where a size is no multiple of 128 the last block holds what is left.  A block of
+ * values v is stored with the scale s = max(max |v| / 448, 2^-126) as v / s rounded to nearest even; a
+ * block that holds an infinity or a NaN gets a NaN scale and NaN values throughout. */
+
+/* Residual addition and Norm with an 8-bit result: h = x + resid, rounded to dtype and stored in
+ * resid_out, then y = g * h / sqrt(mean(h^2) + eps) per row in the 8-bit form.  resid NULL (and then
+ * resid_out NULL): h = x.
+ *  x, resid, resid_out [M, D], g [D] of dtype (AF_BF16 or AF_F32); q [M, D] e4m3;
+ *  scales fp32 [M, ceil(D / 128)].  resid_out may be resid or x itself; no other overlap.
+ * Any M and D >= 1 and any alignment of the element types; M of 2^23 or more is AF_ERR_UNSUPPORTED. */
+af_status af_op_add_rmsnorm_fp8(int32_t dtype, const void* x, const void* resid, const void* g, void* resid_out,
+                                void* q, float* scales, int32_t M, int32_t D, float eps, void* hip_stream);
+
+/* x [M, K] of dtype in the 8-bit form with blocks of block_rows (1 or 128) x 128: q [M, K] e4m3, scales
+ * fp32 [ceil(M / block_rows), ceil(K / 128)].  Any M and K >= 1 and any alignment of the element types;
+ * more blocks than one launch takes (2^28 of 1 x 128, 2^24 of 128 x 128) are AF_ERR_UNSUPPORTED. */
+af_status af_op_quantize_fp8(int32_t dtype, const void* x, void* q, float* scales, int32_t M, int32_t K,
+                             int32_t block_rows, void* hip_stream);
+
+/* Projection y [M, N] = x [M, K] . w [N, K]^T of 8-bit x (xq, xs with blocks of 1 x 128) and w (wq, ws
+ * with blocks of 128 x 128), accumulated in fp32, y of out_dtype (AF_BF16 or AF_F32).  The sums over a
+ * block are taken before its scales are applied, and a row's result does not depend on the other rows
+ * except through the order of the sum over blocks, which goes by the sizes.
+ * Any M and N >= 1.  K % 16 != 0, xq or wq not aligned to 16 bytes, K > 2^22 or more than 2^24 tiles of
+ * 16 x 16 results are AF_ERR_UNSUPPORTED. */
+af_status af_op_linear_fp8(const void* xq, const float* xs, const void* wq, const float* ws, void* y,
+                           int32_t out_dtype, int32_t M, int32_t N, int32_t K, void* hip_stream);
+
+/* Draws one token per row of logits [n_rows, vocab] (AF_BF16 or AF_F32) from given random numbers.
+ * Order a row's tokens by logit, descending, equal ones by index, with weights
+ * w = exp((z - max z) / temperature).  Kept are the first top_k tokens; of these the shortest prefix
+ * whose weight is at least top_p of theirs; of these the ones with w >= min_p.  The first token is
+ * always kept.  The token drawn is the lowest index i at which the kept weight of the indices 0..i
+ * exceeds uniform times all of it.
+ *  temperature, top_k, top_p, min_p: one value per row, or NULL for none (temperature 1, the rest
+ *  off).  temperature <= 0 (or NaN): the greedy token; top_k <= 0, top_p >= 1 (or NaN), min_p <= 0
+ *  (or NaN): off; top_p <= 0: the first token; min_p > 1 counts as 1.
+ *  uniforms [n_rows] in [0, 1); below it counts as 0, 1 and above draw the last kept token.
+ *  tokens   [n_rows].
+ * A logit of -inf or NaN is never drawn; a row that has no other gives token 0, as the greedy head
+ * does.  Logits of +inf share the row.  Weights below 2^-41 count as 0.  The sums are exact, so a
+ * row's token depends on nothing but that row.  vocab > 2^22 or n_rows of 2^22 or more is
+ * AF_ERR_UNSUPPORTED. */
+af_status af_op_sample(int32_t dtype, const void* logits, int32_t n_rows, int32_t vocab, const float* temperature,
+                       const int32_t* top_k, const float* top_p, const float* min_p, const float* uniforms,
+                       int32_t* tokens, void* hip_stream);
+
 /* ------------------------------------------------------------------ timing
  * Kernel classes for per-kernel timing with HIP events recorded on the launch stream. */
 typedef enum af_kernel_class {

@@ -93,6 +93,10 @@ def _load():
         "af_op_gate_up_swiglu": (I32, [P, I32, P, P, I32, P]),
         "af_op_down_residual": (I32, [P, I32, P, P, I32, P]),
         "af_op_lm_head_argmax": (I32, [P, P, I32, SEG, I32, P, P, P]),
+        "af_op_add_rmsnorm_fp8": (I32, [I32, P, P, P, P, P, P, I32, I32, F32, P]),
+        "af_op_quantize_fp8": (I32, [I32, P, P, P, I32, I32, I32, P]),
+        "af_op_linear_fp8": (I32, [P, P, P, P, P, I32, I32, I32, I32, P]),
+        "af_op_sample": (I32, [I32, P, I32, I32, P, P, P, P, P, P, P]),
         "af_weights_set_options": (I32, [P, U32]),
         "af_timing_enable": (I32, [P, U32]),
         "af_timing_read": (I32, [P, C.POINTER(C.c_double), C.POINTER(I64)]),
@@ -338,3 +342,101 @@ def op_lm_head_argmax(w: Weights, hidden, segs, out_logits=None, out_tokens=None
     sa = segments_array(segs)
     _check(lib.af_op_lm_head_argmax(w.h, _ptr(hidden), hidden.shape[0], sa, len(sa), _ptr(out_logits),
                                     _ptr(out_tokens), _stream(stream)))
+
+
+# ----------------------------------------------------------------------------- 8-bit projections and sampling
+FP8 = torch.float8_e4m3fn
+FP8_BLOCK = 128  # columns (and, for weights, rows) that share a scale
+
+
+def _want(what: str, t: torch.Tensor, shape, dtype, device):
+    """Refuses a tensor that the library would read or write outside of, or as another type."""
+    if t.shape != shape or t.dtype != dtype or t.device != device or not t.is_contiguous():
+        raise ValueError(f"{what} must be a contiguous {dtype} tensor of shape {tuple(shape)} on {device}, "
+                         f"got {t.dtype} {tuple(t.shape)} on {t.device}")
+
+
+def _call_on(device: torch.device, stream, fn, *args):
+    """Calls the library with ``device`` current, on its current stream unless one is given."""
+    if device.type != "cuda":
+        raise ValueError(f"tensors must be on a GPU, got {device}")
+    if device.index != torch.cuda.current_device():
+        with torch.cuda.device(device):
+            return _call_on(device, stream, fn, *args)
+    _check(fn(*args, (torch.cuda.current_stream(device) if stream is None else stream).cuda_stream))
+
+
+def fp8_blocks(n: int) -> int:
+    """Blocks of 128 that n columns or rows take."""
+    return -(-n // FP8_BLOCK)
+
+
+def op_add_rmsnorm_fp8(x: torch.Tensor, resid: Optional[torch.Tensor], g: torch.Tensor,
+                       resid_out: Optional[torch.Tensor], q: torch.Tensor, scales: torch.Tensor, eps: float,
+                       stream=None):
+    """resid_out <- x + resid (both None: x alone), then its RMSNorm as e4m3 ``q`` [M, D] with fp32
+    ``scales`` [M, ceil(D / 128)].  resid_out may be resid or x."""
+    M, D = x.shape
+    dt, dev = x.dtype, x.device
+    _want("x", x, (M, D), dt, dev)
+    _want("g", g, (D,), dt, dev)
+    _want("q", q, (M, D), FP8, dev)
+    _want("scales", scales, (M, fp8_blocks(D)), torch.float32, dev)
+    if (resid is None) != (resid_out is None):
+        raise ValueError("resid and resid_out go together: both or neither")
+    if resid is not None:
+        _want("resid", resid, (M, D), dt, dev)
+        _want("resid_out", resid_out, (M, D), dt, dev)
+    _call_on(dev, stream, lib.af_op_add_rmsnorm_fp8, dtype_code(dt), x.data_ptr(),
+             None if resid is None else resid.data_ptr(), g.data_ptr(),
+             None if resid is None else resid_out.data_ptr(), q.data_ptr(), scales.data_ptr(), M, D, eps)
+
+
+def op_quantize_fp8(x: torch.Tensor, q: torch.Tensor, scales: torch.Tensor, block_rows: int = 1, stream=None):
+    """x [M, K] as e4m3 ``q`` with an fp32 scale per block of ``block_rows`` (1: activations, 128:
+    weights) x 128: ``scales`` [ceil(M / block_rows), ceil(K / 128)]."""
+    M, K = x.shape
+    dev = x.device
+    if block_rows not in (1, FP8_BLOCK):
+        raise ValueError("block_rows must be 1 or 128")
+    _want("x", x, (M, K), x.dtype, dev)
+    _want("q", q, (M, K), FP8, dev)
+    _want("scales", scales, (M if block_rows == 1 else fp8_blocks(M), fp8_blocks(K)), torch.float32, dev)
+    _call_on(dev, stream, lib.af_op_quantize_fp8, dtype_code(x.dtype), x.data_ptr(), q.data_ptr(), scales.data_ptr(),
+             M, K, block_rows)
+
+
+def op_linear_fp8(xq: torch.Tensor, xs: torch.Tensor, wq: torch.Tensor, ws: torch.Tensor, y: torch.Tensor,
+                  stream=None):
+    """y [M, N] (bf16 or fp32) = x . w^T of e4m3 ``xq`` [M, K] with scales ``xs`` [M, ceil(K / 128)] and
+    ``wq`` [N, K] with ``ws`` [ceil(N / 128), ceil(K / 128)]; K a multiple of 16."""
+    (M, K), N = xq.shape, wq.shape[0]
+    dev, kb = xq.device, fp8_blocks(K)
+    _want("xq", xq, (M, K), FP8, dev)
+    _want("wq", wq, (N, K), FP8, dev)
+    _want("xs", xs, (M, kb), torch.float32, dev)
+    _want("ws", ws, (fp8_blocks(N), kb), torch.float32, dev)
+    _want("y", y, (M, N), y.dtype, dev)
+    _call_on(dev, stream, lib.af_op_linear_fp8, xq.data_ptr(), xs.data_ptr(), wq.data_ptr(), ws.data_ptr(),
+             y.data_ptr(), dtype_code(y.dtype), M, N, K)
+
+
+def op_sample(logits: torch.Tensor, uniforms: torch.Tensor, tokens: torch.Tensor,
+              temperature: Optional[torch.Tensor] = None, top_k: Optional[torch.Tensor] = None,
+              top_p: Optional[torch.Tensor] = None, min_p: Optional[torch.Tensor] = None, stream=None):
+    """One token per row of ``logits`` [n, vocab] (bf16 or fp32) into ``tokens`` (int32 [n]), drawn with
+    the fp32 numbers ``uniforms`` [n] in [0, 1).  Settings are per-row tensors (fp32, ``top_k`` int32) or
+    None: temperature (0: greedy), top_k (0: off), top_p (1: off), min_p (0: off), applied in this order."""
+    n, V = logits.shape
+    dev, row, f32 = logits.device, (n,), torch.float32
+    _want("logits", logits, (n, V), logits.dtype, dev)
+    _want("uniforms", uniforms, row, f32, dev)
+    _want("tokens", tokens, row, torch.int32, dev)
+    at = []
+    for what, t, dt in (("temperature", temperature, f32), ("top_k", top_k, torch.int32), ("top_p", top_p, f32),
+                        ("min_p", min_p, f32)):
+        if t is not None:
+            _want(what, t, row, dt, dev)
+        at.append(None if t is None else t.data_ptr())
+    _call_on(dev, stream, lib.af_op_sample, dtype_code(logits.dtype), logits.data_ptr(), n, V, *at,
+             uniforms.data_ptr(), tokens.data_ptr())

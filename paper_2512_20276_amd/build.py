@@ -13,8 +13,9 @@ CSRC = os.path.join(PKG, "csrc")
 OUT = os.path.join(PKG, "libactionflow.so")
 BUILD_DIR = os.path.join(PKG, "_build")
 
-HIP_SOURCES = ["af_gemm.hip", "af_stream.hip", "af_gemm_wide.hip", "af_gemm_f32.hip", "af_attention.hip", "af_kernels.hip", "af_noalloc.hip"]
-HOST_SOURCES = ["af_ring.cpp", "af_model.cpp"]
+HIP_SOURCES = ["af_gemm.hip", "af_stream.hip", "af_gemm_wide.hip", "af_gemm_f32.hip", "af_attention.hip", "af_kernels.hip", "af_noalloc.hip",
+               "af_fp8.hip", "af_gemm_fp8.hip", "af_sample.hip"]
+HOST_SOURCES = ["af_ring.cpp", "af_model.cpp", "af_ops.cpp"]
 
 # Packed-fp32 instructions are disabled for all device code (hipcc makes them from plain float
 # code otherwise); the host pass warns that it does not know the feature, which is harmless.
@@ -38,7 +39,7 @@ def _run(cmd):
 
 
 HEADERS = [os.path.join(CSRC, "af_internal.h"), os.path.join(CSRC, "af_device.h"),
-           os.path.join(CSRC, "af_epilogue.h"),
+           os.path.join(CSRC, "af_epilogue.h"), os.path.join(CSRC, "af_fp8.h"),
            os.path.join(ROOT, "include", "actionflow.h")]
 
 
