@@ -349,21 +349,25 @@ FP8 = torch.float8_e4m3fn
 FP8_BLOCK = 128  # columns (and, for weights, rows) that share a scale
 
 
-def _want(what: str, t: torch.Tensor, shape, dtype, device):
+def _want(what: str, t: torch.Tensor, shape, dtype, device: int):
     """Refuses a tensor that the library would read or write outside of, or as another type."""
-    if t.shape != shape or t.dtype != dtype or t.device != device or not t.is_contiguous():
-        raise ValueError(f"{what} must be a contiguous {dtype} tensor of shape {tuple(shape)} on {device}, "
-                         f"got {t.dtype} {tuple(t.shape)} on {t.device}")
+    if t.dtype is not dtype or t.shape != shape or t.get_device() != device or not t.is_contiguous():
+        raise ValueError(f"{what} must be a contiguous {dtype} tensor of shape {tuple(shape)} on "
+                         f"{'the CPU' if device < 0 else f'cuda:{device}'}, got {t.dtype} {tuple(t.shape)} on {t.device}")
 
 
-def _call_on(device: torch.device, stream, fn, *args):
-    """Calls the library with ``device`` current, on its current stream unless one is given."""
-    if device.type != "cuda":
-        raise ValueError(f"tensors must be on a GPU, got {device}")
-    if device.index != torch.cuda.current_device():
+def _call_on(device: int, stream, fn, *args):
+    """Calls the library with GPU ``device`` current, on its current stream unless one is given."""
+    if device < 0:
+        raise ValueError("tensors must be on a GPU")
+    if device != torch.cuda.current_device():
         with torch.cuda.device(device):
             return _call_on(device, stream, fn, *args)
-    _check(fn(*args, (torch.cuda.current_stream(device) if stream is None else stream).cuda_stream))
+    # the raw handle: building a Stream object for it takes as long as the launch
+    handle = torch._C._cuda_getCurrentRawStream(device) if stream is None else stream.cuda_stream
+    code = fn(*args, handle)
+    if code != AF_OK:
+        _check(code)
 
 
 def fp8_blocks(n: int) -> int:
@@ -377,7 +381,7 @@ def op_add_rmsnorm_fp8(x: torch.Tensor, resid: Optional[torch.Tensor], g: torch.
     """resid_out <- x + resid (both None: x alone), then its RMSNorm as e4m3 ``q`` [M, D] with fp32
     ``scales`` [M, ceil(D / 128)].  resid_out may be resid or x."""
     M, D = x.shape
-    dt, dev = x.dtype, x.device
+    dt, dev = x.dtype, x.get_device()
     _want("x", x, (M, D), dt, dev)
     _want("g", g, (D,), dt, dev)
     _want("q", q, (M, D), FP8, dev)
@@ -396,7 +400,7 @@ def op_quantize_fp8(x: torch.Tensor, q: torch.Tensor, scales: torch.Tensor, bloc
     """x [M, K] as e4m3 ``q`` with an fp32 scale per block of ``block_rows`` (1: activations, 128:
     weights) x 128: ``scales`` [ceil(M / block_rows), ceil(K / 128)]."""
     M, K = x.shape
-    dev = x.device
+    dev = x.get_device()
     if block_rows not in (1, FP8_BLOCK):
         raise ValueError("block_rows must be 1 or 128")
     _want("x", x, (M, K), x.dtype, dev)
@@ -411,7 +415,7 @@ def op_linear_fp8(xq: torch.Tensor, xs: torch.Tensor, wq: torch.Tensor, ws: torc
     """y [M, N] (bf16 or fp32) = x . w^T of e4m3 ``xq`` [M, K] with scales ``xs`` [M, ceil(K / 128)] and
     ``wq`` [N, K] with ``ws`` [ceil(N / 128), ceil(K / 128)]; K a multiple of 16."""
     (M, K), N = xq.shape, wq.shape[0]
-    dev, kb = xq.device, fp8_blocks(K)
+    dev, kb = xq.get_device(), fp8_blocks(K)
     _want("xq", xq, (M, K), FP8, dev)
     _want("wq", wq, (N, K), FP8, dev)
     _want("xs", xs, (M, kb), torch.float32, dev)
@@ -428,7 +432,7 @@ def op_sample(logits: torch.Tensor, uniforms: torch.Tensor, tokens: torch.Tensor
     the fp32 numbers ``uniforms`` [n] in [0, 1).  Settings are per-row tensors (fp32, ``top_k`` int32) or
     None: temperature (0: greedy), top_k (0: off), top_p (1: off), min_p (0: off), applied in this order."""
     n, V = logits.shape
-    dev, row, f32 = logits.device, (n,), torch.float32
+    dev, row, f32 = logits.get_device(), (n,), torch.float32
     _want("logits", logits, (n, V), logits.dtype, dev)
     _want("uniforms", uniforms, row, f32, dev)
     _want("tokens", tokens, row, torch.int32, dev)

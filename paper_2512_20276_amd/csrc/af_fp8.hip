@@ -4,7 +4,13 @@
 // A block of values v is stored as q = e4m3(v / s) with s = max(max |v| / 448, 2^-126), rounded to
 // nearest even: the largest magnitude lands on 448, the largest e4m3 value, and the floor keeps the
 // division defined for a block of zeros.  A block that holds an infinity or a NaN gets s = NaN and
-// q = NaN throughout, so that nothing computed from it looks finite.
+// q = NaN throughout, so that nothing computed from it looks finite.  The quotient is v times the
+// reciprocal instruction's 1 / s, within 2^-22 of the exact one: an element within that of the middle
+// between two e4m3 values (one in 10^6) may take either.  (With the division itself, ten instructions an
+// element, 22016 x 4096 weights took 59.5 us, bound by them.)
+//
+// Every kernel here reads its input once, in 16-byte accesses, and is bound by memory: what it holds of a
+// block or a row stays in registers between the maximum, or the norm, and the rounding.
 #include "af_device.h"
 #include "af_fp8.h"
 
@@ -21,27 +27,37 @@ __device__ __forceinline__ float scale_of(unsigned largest) {
   return fmaxf(__uint_as_float(largest) / FP8_MAX, FP8_MIN_SCALE);
 }
 
+// The lane's value rotated by N places within its row of 16 lanes.
+template <int N>
+__device__ __forceinline__ unsigned ror16(unsigned v) {
+  return (unsigned)__builtin_amdgcn_update_dpp(0, (int)v, 0x120 + N, 0xf, 0xf, false);
+}
 // Maximum over the 16 lanes (of 8 values each) that hold one block of 128.
 __device__ __forceinline__ unsigned max16(unsigned m) {
-#pragma unroll
-  for (int o = 8; o > 0; o >>= 1) m = max(m, (unsigned)__shfl_xor((int)m, o));
-  return m;
+  m = max(m, ror16<8>(m));
+  m = max(m, ror16<4>(m));
+  m = max(m, ror16<2>(m));
+  return max(m, ror16<1>(m));
+}
+// Sum over the wave, in one order (every kernel that normalises a row takes the same).
+__device__ __forceinline__ float wave_sum(float v) {
+  v += __uint_as_float(ror16<8>(__float_as_uint(v)));
+  v += __uint_as_float(ror16<4>(__float_as_uint(v)));
+  v += __uint_as_float(ror16<2>(__float_as_uint(v)));
+  v += __uint_as_float(ror16<1>(__float_as_uint(v)));
+  v += __shfl_xor(v, 16);
+  return v + __shfl_xor(v, 32);
 }
 
-// Eight values as e4m3, in order.
+// Eight values over the scale s, as e4m3, in order.
 __device__ __forceinline__ uint2 pack8(const float* v, float s) {
-  float t[8];
-#pragma unroll
-  for (int e = 0; e < 8; ++e) t[e] = v[e] / s;
-  uint2 r;
+  const float r = __builtin_amdgcn_rcpf(s);
   int lo = 0, hi = 0;
-  lo = __builtin_amdgcn_cvt_pk_fp8_f32(t[0], t[1], lo, false);
-  lo = __builtin_amdgcn_cvt_pk_fp8_f32(t[2], t[3], lo, true);
-  hi = __builtin_amdgcn_cvt_pk_fp8_f32(t[4], t[5], hi, false);
-  hi = __builtin_amdgcn_cvt_pk_fp8_f32(t[6], t[7], hi, true);
-  r.x = (unsigned)lo;
-  r.y = (unsigned)hi;
-  return r;
+  lo = __builtin_amdgcn_cvt_pk_fp8_f32(v[0] * r, v[1] * r, lo, false);
+  lo = __builtin_amdgcn_cvt_pk_fp8_f32(v[2] * r, v[3] * r, lo, true);
+  hi = __builtin_amdgcn_cvt_pk_fp8_f32(v[4] * r, v[5] * r, hi, false);
+  hi = __builtin_amdgcn_cvt_pk_fp8_f32(v[6] * r, v[7] * r, hi, true);
+  return make_uint2((unsigned)lo, (unsigned)hi);
 }
 
 // Eight consecutive elements of a row of which n (1..8, or fewer: none) exist; the rest are zeros.
@@ -76,74 +92,137 @@ __device__ __forceinline__ void store_q(uint8_t* p, int n, uint2 q) {
 }
 
 // ------------------------------------------------------------------ residual + RMSNorm -> e4m3
-// One workgroup per row; 16 consecutive threads hold one block of 128 columns.
-constexpr int NORM8_THREADS = 512;
-
-template <typename T>
-__global__ __launch_bounds__(NORM8_THREADS) void add_rmsnorm_fp8_kernel(const T* x, const T* resid,
-                                                                      const T* __restrict__ g, T* resid_out,
-                                                                      uint8_t* __restrict__ q,
-                                                                      float* __restrict__ scales, int D, int kb,
-                                                                      float eps) {
-  __shared__ float red[NORM8_THREADS / 64];
-  const size_t row = blockIdx.x;
-  const T* xr = x + row * D;
-  const T* rr = resid ? resid + row * D : nullptr;
-  T* hr = resid ? resid_out + row * D : nullptr;
+// WAVES waves to a row: one (rows of up to 512 columns, four rows a workgroup) or eight, CPL chunks of 8
+// columns a thread, 16 consecutive lanes to a block of 128 columns.  The row stays in registers; a workgroup
+// that has another row to do requests it before it waits for this one's sum.  CPL = 0: longer rows, whose
+// second pass reads back what the thread itself wrote (or the input).
+// A row is added up in one order, whatever the number of rows.
+template <typename T, int WAVES, int CPL>
+__global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void add_rmsnorm_fp8_kernel(
+    const T* x, const T* resid, const T* __restrict__ g, T* resid_out, uint8_t* __restrict__ q,
+    float* __restrict__ scales, int M, int D, int kb, float eps) {
+  constexpr int RPW = WAVES == 1 ? 4 : 1;  // rows of a workgroup at a time
+  __shared__ float red[2][8];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int c0 = WAVES == 1 ? lane : (int)threadIdx.x;
+  constexpr int STEP = 64 * WAVES;
   const int n_ch = kb * 16;  // chunks of 8 columns, whole blocks of them
-  float ss = 0.f;
-  for (int c = threadIdx.x; c < n_ch; c += NORM8_THREADS) {
+
+  auto quantize = [&](size_t row, int c, const T* h, const T* gv, float inv) {
     const int n = D - 8 * c;
-    T v[8];
-    load_chunk(xr + 8 * c, n, v);
-    if (resid) {
-      T r[8];
-      load_chunk(rr + 8 * c, n, r);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] = from_f<T>(to_f(v[e]) + to_f(r[e]));
-      store_chunk(hr + 8 * c, n, v);
-    }
-#pragma unroll
-    for (int e = 0; e < 8; ++e) ss = fmaf(to_f(v[e]), to_f(v[e]), ss);
-  }
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) ss += __shfl_xor(ss, o);
-  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = ss;
-  __syncthreads();
-  float tot = red[0];
-#pragma unroll
-  for (int w = 1; w < NORM8_THREADS / 64; ++w) tot += red[w];
-  const float inv = 1.0f / sqrtf(tot / (float)D + eps);
-  const T* src = resid ? hr : xr;  // each thread reads back what it wrote
-  for (int c = threadIdx.x; c < n_ch; c += NORM8_THREADS) {
-    const int n = D - 8 * c;
-    T v[8], gv[8];
-    load_chunk(src + 8 * c, n, v);
-    load_chunk(g + 8 * c, n, gv);
     float y[8];
     unsigned m = 0;
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      y[e] = to_f(v[e]) * inv * to_f(gv[e]);
-      if (e < n) m = max(m, abs_bits(y[e]));
-      else y[e] = 0.f;
+      y[e] = e < n ? to_f(h[e]) * inv * to_f(gv[e]) : 0.f;
+      m = max(m, abs_bits(y[e]));
     }
     const float s = scale_of(max16(m));
     if (n > 0) store_q(q + row * D + 8 * c, n, pack8(y, s));
     if ((c & 15) == 0) scales[row * kb + (c >> 4)] = s;
+  };
+  // 1 / the root of the mean square, from this thread's part of the sum
+  auto norm_of = [&](float ss, int turn) {
+    ss = wave_sum(ss);
+    if constexpr (WAVES > 1) {
+      if (lane == 0) red[turn][wave] = ss;
+      __syncthreads();
+      ss = red[turn][0];
+#pragma unroll
+      for (int w = 1; w < WAVES; ++w) ss += red[turn][w];
+    }
+    return 1.0f / sqrtf(ss / (float)D + eps);
+  };
+
+  if constexpr (CPL > 0) {
+    T h[CPL][8], r[CPL][8], gv[CPL][8];
+    const size_t step = (size_t)gridDim.x * RPW;
+    size_t row = (size_t)blockIdx.x * RPW + (WAVES == 1 ? wave : 0);
+    auto load = [&](size_t row) {
+#pragma unroll
+      for (int i = 0; i < CPL; ++i) {
+        const int c = c0 + STEP * i, n = row < (size_t)M ? D - 8 * c : 0;
+        load_chunk(x + row * D + 8 * c, n, h[i]);
+        if (resid) load_chunk(resid + row * D + 8 * c, n, r[i]);
+      }
+    };
+    load(row);
+#pragma unroll
+    for (int i = 0; i < CPL; ++i) load_chunk(g + 8 * (c0 + STEP * i), D - 8 * (c0 + STEP * i), gv[i]);
+    for (int turn = 0; row < (size_t)M; row += step, turn ^= 1) {  // a wave's rows are the same for all its lanes
+      T v[CPL][8];
+      float ss = 0.f;
+#pragma unroll
+      for (int i = 0; i < CPL; ++i) {
+        const int c = c0 + STEP * i, n = D - 8 * c;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          v[i][e] = resid ? from_f<T>(to_f(h[i][e]) + to_f(r[i][e])) : h[i][e];
+          ss = fmaf(to_f(v[i][e]), to_f(v[i][e]), ss);
+        }
+        if (resid && n > 0) store_chunk(resid_out + row * D + 8 * c, n, v[i]);
+      }
+      load(row + step);
+      const float inv = norm_of(ss, turn);
+#pragma unroll
+      for (int i = 0; i < CPL; ++i)
+        if (c0 + STEP * i < n_ch) quantize(row, c0 + STEP * i, v[i], gv[i], inv);
+    }
+  } else {
+    const size_t row = blockIdx.x;
+    const T* xr = x + row * D;
+    T* hr = resid ? resid_out + row * D : nullptr;
+    float ss = 0.f;
+    for (int c = c0; c < n_ch; c += STEP) {
+      const int n = D - 8 * c;
+      T h[8];
+      load_chunk(xr + 8 * c, n, h);
+      if (resid) {
+        T r[8];
+        load_chunk(resid + row * D + 8 * c, n, r);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) h[e] = from_f<T>(to_f(h[e]) + to_f(r[e]));
+        store_chunk(hr + 8 * c, n, h);
+      }
+#pragma unroll
+      for (int e = 0; e < 8; ++e) ss = fmaf(to_f(h[e]), to_f(h[e]), ss);
+    }
+    const float inv = norm_of(ss, 0);
+    const T* src = resid ? hr : xr;
+    for (int c = c0; c < n_ch; c += STEP) {
+      T h[8], gv[8];
+      load_chunk(src + 8 * c, D - 8 * c, h);
+      load_chunk(g + 8 * c, D - 8 * c, gv);
+      quantize(row, c, h, gv, inv);
+    }
   }
+}
+
+// Workgroups of eight waves, three a CU (2264 x 4096 bf16: 14.6 us; two 15.4, four 16.1, one row each 15.2).
+constexpr int NORM8_WGS = 768;
+
+template <typename T>
+static hipError_t norm_launch(const T* x, const T* resid, const T* g, T* resid_out, uint8_t* q, float* scales, int M,
+                              int D, float eps, hipStream_t s) {
+  const int kb = fp8_blocks(D);
+  const dim3 few((unsigned)std::min((M + 3) / 4, 2 * NORM8_WGS)), some((unsigned)std::min(M, NORM8_WGS)), all((unsigned)M);
+  if (D <= 512)
+    hipLaunchKernelGGL((add_rmsnorm_fp8_kernel<T, 1, 1>), few, dim3(256), 0, s, x, resid, g, resid_out, q, scales, M, D, kb, eps);
+  else if (D <= 4096)
+    hipLaunchKernelGGL((add_rmsnorm_fp8_kernel<T, 8, 1>), some, dim3(512), 0, s, x, resid, g, resid_out, q, scales, M, D, kb, eps);
+  else if (D <= 12288)
+    hipLaunchKernelGGL((add_rmsnorm_fp8_kernel<T, 8, 3>), some, dim3(512), 0, s, x, resid, g, resid_out, q, scales, M, D, kb, eps);
+  else
+    hipLaunchKernelGGL((add_rmsnorm_fp8_kernel<T, 8, 0>), all, dim3(512), 0, s, x, resid, g, resid_out, q, scales, M, D, kb, eps);
+  return hipGetLastError();
 }
 
 hipError_t launch_add_rmsnorm_fp8(int dtype, const void* x, const void* resid, const void* g, void* resid_out,
                                   void* q, float* scales, int M, int D, float eps, hipStream_t s) {
-  const int kb = fp8_blocks(D);
-  if (dtype == AF_BF16)
-    hipLaunchKernelGGL(add_rmsnorm_fp8_kernel<bf16>, dim3(M), dim3(NORM8_THREADS), 0, s, (const bf16*)x,
-                       (const bf16*)resid, (const bf16*)g, (bf16*)resid_out, (uint8_t*)q, scales, D, kb, eps);
-  else
-    hipLaunchKernelGGL(add_rmsnorm_fp8_kernel<float>, dim3(M), dim3(NORM8_THREADS), 0, s, (const float*)x,
-                       (const float*)resid, (const float*)g, (float*)resid_out, (uint8_t*)q, scales, D, kb, eps);
-  return hipGetLastError();
+  return dtype == AF_BF16 ? norm_launch((const bf16*)x, (const bf16*)resid, (const bf16*)g, (bf16*)resid_out,
+                                        (uint8_t*)q, scales, M, D, eps, s)
+                          : norm_launch((const float*)x, (const float*)resid, (const float*)g, (float*)resid_out,
+                                        (uint8_t*)q, scales, M, D, eps, s);
 }
 
 // ------------------------------------------------------------------ quantisation
