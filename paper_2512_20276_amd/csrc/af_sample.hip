@@ -10,13 +10,26 @@
 // that a sum over a long vocabulary still tells neighbouring tokens apart (an fp32 sum of 32000 weights
 // is off by more than the share of most of them).  Tokens below 2^-41 of the top one weigh nothing.
 //
-// One workgroup of 1024 threads per row, which holds up to 32768 logits in registers, so that a row is
-// read once (longer ones are read again, from L2, in every pass).  Nothing is sorted:
+// One workgroup of 1024 threads per row, which keeps a row of up to 32768 logits in LDS, so that memory
+// is read once (longer ones are read again in every pass, 48 KB of a row under way at a time).  Passes are
+// loops over chunks of 16 bytes a thread: with the row in registers they were unrolled 32 times, and
+// fetching those instructions took longer than executing them (64 rows of 32000 fp32 logits, top_p alone:
+// 45.6 us, as loops 36.5).
+// Nothing is sorted:
 //  - top-k of up to 1024: 1024 threads hold a maximum each; the k-th largest of those is a bound that at
 //    least k tokens reach and hardly more do.  A histogram of the maxima gives it, the tokens past it
 //    (some 50 to 70 for k = 50) meet in LDS, and everything else happens among them.
 //  - otherwise a cut is found by a histogram of counts or weights over the distance from the top, in
-//    bins of 1/128 of that distance, then again within the bin that holds the cut until it is one value.
+//    bins of 1/128 of that distance (fp32 rows in LDS, where no more bins fit) or 1/256 (256 rows of 131072
+//    bf16 logits, top_p alone: 211 us with 128 bins to an octave, which hold several values of many equal
+//    logits each, 176 with 256); the tokens of the bin that holds it are put into order where they
+//    are few, else the bin is divided again.
+// Bound: with top_k, reading the row and the chain of some ten barriers (64 x 32000 fp32, k = 50: 12.2 us;
+// the read alone is 1.5 us over the whole card, but 64 of 256 CUs have a row); else the 64-bit weights,
+// some 25 instructions a token and pass on the one CU that has the row (64 x 32000 fp32: 15.4 us with
+// temperature alone, 36.5 with top_p; 256 x 131072 bf16: 53.6 and 176).  A row stays on one CU, since
+// sharing it needs a wait between workgroups and these calls come behind a projection that costs more.
+
 #include "af_device.h"
 #include "af_fp8.h"
 
@@ -24,9 +37,8 @@ namespace af {
 
 constexpr int SAMPLE_THREADS = 1024;
 constexpr int SAMPLE_WAVES = SAMPLE_THREADS / 64;
-constexpr int SAMPLE_PER = 32;                            // logits of a thread in registers
-constexpr int SAMPLE_TILE = SAMPLE_THREADS * SAMPLE_PER;  // logits of a workgroup in registers
-constexpr int SAMPLE_BINS = 4 * SAMPLE_THREADS;
+constexpr int SAMPLE_HELD = 32768;                        // logits of a row that is kept in LDS
+constexpr int SAMPLE_FEW = 256;                           // tokens of a bin that are put into order
 constexpr int SAMPLE_EXP = 64;                            // entries of the table of powers of two
 typedef unsigned long long u64;
 
@@ -42,16 +54,22 @@ __device__ __forceinline__ unsigned key_of(float z) {
 __device__ __forceinline__ float value_of(unsigned key) {
   return __uint_as_float(key & 0x80000000u ? key & 0x7fffffffu : ~key);
 }
-// Bin of a distance d >= 0 between keys: 128 to an octave.
-__device__ __forceinline__ int bin_of(unsigned d) {
-  const int b = (int)(__float_as_uint((float)d) >> 16) - (127 << 7);
-  return d == 0 ? 0 : b;  // d = 1: bin 0 too
-}
-// A distance that no element of bins 0 .. b exceeds (the conversion may have rounded it down).
-__device__ __forceinline__ unsigned reach_of(int b) {
-  const float f = __uint_as_float(((unsigned)(b + (127 << 7)) << 16) | 0xffffu);
-  return f >= 4294966784.f ? 0xffffffffu : (unsigned)(f * 1.0000005f) + 1u;
-}
+// Bins of a distance d >= 0 between keys, 2^BITS to an octave from 2^16 on (the bits behind the leading
+// one); nearer ones share bin 0.  BINS of them in all.
+template <int BITS>
+struct Bins {
+  static constexpr int BINS = 16 << BITS;
+  static __device__ __forceinline__ int of(unsigned d) {
+    d = max(d, 0x10000u);
+    const int z = __clz((int)d);
+    return (int)(d << z >> (31 - BITS)) + ((15 - z) << BITS) - (1 << BITS);
+  }
+  // The smallest and the largest distance of a bin.
+  static __device__ __forceinline__ unsigned first(int bin) {
+    return bin == 0 ? 0u : ((1u << BITS) + (bin & ((1 << BITS) - 1))) << ((bin >> BITS) + 16 - BITS);
+  }
+  static __device__ __forceinline__ unsigned last(int bin) { return bin >= BINS - 1 ? 0xffffffffu : first(bin + 1) - 1u; }
+};
 
 // ------------------------------------------------------------------ sums over lanes
 // The lane's value moved by a DPP control; lanes without a source, or in rows masked out, get 0.
@@ -78,140 +96,204 @@ __device__ __forceinline__ u64 readlane64(u64 v, int lane) {
          (unsigned)__builtin_amdgcn_readlane((int)(unsigned)v, lane);
 }
 
+// The row (or nothing) and the histogram, in as many copies, by lane, as there is room for: tokens of a bin
+// that meet in one instruction are added one after the other, and bf16 logits have few values.
+template <int ROW_BYTES, int BINS, int COPIES>
 struct SampleLds {
-  u64 hist[SAMPLE_BINS];
+  uint4 tile[ROW_BYTES / 16 + 1];
+  u64 hist[BINS * COPIES];
   u64 cand[SAMPLE_THREADS];
   double exp2[SAMPLE_EXP];
-  u64 red[2][SAMPLE_WAVES];
+  u64 part[SAMPLE_WAVES], red[2][SAMPLE_WAVES];
   float redf[SAMPLE_WAVES];
-  u64 left, tile_total[SAMPLE_MAX_V / SAMPLE_TILE];
+  u64 left;
   unsigned lo, hi;
   int bin, n, at;
 };
 
-// Sum over the threads before this one, and over all.  (turn: which of two sets of sums in LDS; a set is
-// free for the call after next, since every call has a barrier.)
-__device__ __forceinline__ u64 block_scan(u64 v, SampleLds& l, int turn, u64* total) {
-  const u64 x = wave_scan(v);
-  const int wave = threadIdx.x >> 6;
-  if ((threadIdx.x & 63) == 63) l.red[turn][wave] = x;
-  __syncthreads();
-  u64 before = 0, all = 0;
-#pragma unroll
-  for (int w = 0; w < SAMPLE_WAVES; ++w) {
-    const u64 t = l.red[turn][w];
-    all += t;
-    before += w < wave ? t : 0;
-  }
-  *total = all;
-  return before + x - v;
+// Largest of the 16 lanes of a row, in all of them.
+template <int N>
+__device__ __forceinline__ float rorf(float v) {
+  return __uint_as_float((unsigned)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(v), 0x120 + N, 0xf, 0xf, false));
+}
+__device__ __forceinline__ float row_max(float v) {
+  v = fmaxf(v, rorf<8>(v));
+  v = fmaxf(v, rorf<4>(v));
+  v = fmaxf(v, rorf<2>(v));
+  return fmaxf(v, rorf<1>(v));
+}
+__device__ __forceinline__ float lane_of(float v, int lane) {
+  return __uint_as_float((unsigned)__builtin_amdgcn_readlane((int)__float_as_uint(v), lane));
 }
 
-// exp((z - top) / T) in units of 2^-40: c = log2(e) / T, powers of two from a table and a polynomial,
-// 2^a = 2^(j / 64) 2^r with |r| <= 1/128, off by less than 1e-13 of itself.
+// Sum over the threads before this one, and over all.  (turn: which of two sets of sums in LDS; a set is
+// free for the call after next, since every call has a barrier.)
+template <class L>
+__device__ __forceinline__ u64 block_scan(u64 v, L& l, int turn, u64* total) {
+  static_assert(SAMPLE_WAVES == 16, "a row of lanes adds the waves up");
+  const u64 x = wave_scan(v);
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  if ((threadIdx.x & 63) == 63) l.red[turn][wave] = x;
+  __syncthreads();
+  const u64 upto = row_scan(l.red[turn][threadIdx.x & 15]);
+  *total = readlane64(upto, 15);
+  return x - v + (wave > 0 ? readlane64(upto, wave - 1) : 0);
+}
+
+// 2^(40 + i / 64)
+__device__ const double EXP2_TABLE[SAMPLE_EXP] = {
+    1099511627776.0, 1111484524408.0237, 1123587797336.3408, 1135822866265.7363,
+    1148191166360.5662, 1160694148413.102, 1173333279013.7073, 1186110040722.8672,
+    1199025932245.0925, 1212082468604.716, 1225281181323.604, 1238623618600.8022,
+    1252111345494.1387, 1265745944103.804, 1279529013757.93, 1293462171200.1902,
+    1307547050779.4426, 1321785304641.4373, 1336178602922.612, 1350728633945.9978,
+    1365437104419.2583, 1380305739634.8853, 1395336283672.5735, 1410530499603.8008,
+    1425890169698.6345, 1441417095634.7908, 1457113098708.9692, 1472980020050.4907,
+    1489019720837.26, 1505234082514.08, 1521625007013.345, 1538194416978.134,
+    1554944255987.7375, 1571876488785.6365, 1588993101509.9658, 1606296101926.4866,
+    1623787519664.0955, 1641469406452.899, 1659343836364.8796, 1677412906057.1829,
+    1695678735018.0535, 1714143465815.4507, 1732809264348.3684, 1751678320100.8945,
+    1770752846399.0352, 1790035080670.3372, 1809527284706.3352, 1829231744927.8591,
+    1849150772653.2297, 1869286704369.3738, 1889641902005.8923, 1910218753212.1138,
+    1931019671637.163, 1952047097213.0808, 1973303496441.0256, 1994791362680.5928,
+    2016513216442.283, 2038471605683.1575, 2060669106105.7107, 2083108321459.9976,
+    2105791883849.0532, 2128722454037.6345, 2151902721764.3281, 2175335406057.0527,
+};
+
+// exp((z - top) / T) in units of 2^-40, c = 64 log2(e) / T: 2^(a / 64) for a = (z - top) c is a power of two
+// times a table's 2^(i / 64) times 2^(r / 64) with |r| <= 1/2 from a polynomial, off by less than 1e-13 of
+// itself.  z and top are not +inf.  Adding 1.5 * 2^52 rounds a to a whole number, which then stands in the sum's low word.
 struct Weigh {
   double top, c;
   const double* table;
   __device__ __forceinline__ u64 operator()(float z) const {
-    const double a = ((double)z - top) * c;
-    if (!(a > -41.5)) return (double)z == top ? (u64)1 << 40 : 0;  // also where both are infinite, or c is
-    const double j = rint(a * 64.0), r = fma(j, -1.0 / 64.0, a);
-    const int n = (int)j;
-    // exp(r ln 2) - 1 to the fourth power
-    double p = fma(r, 9.618129107628477e-3, 5.550410866482158e-2);
-    p = fma(r, p, 2.402265069591007e-1);
-    p = fma(r, p, 6.931471805599453e-1);
-    const double t = table[n & 63];
-    const double w = ldexp(fma(t * r, p, t), 40 + (n >> 6));
-    return (u64)__double_as_longlong(w + 4503599627370496.0) & 0xfffffffffffffULL;  // + 2^52: rounded to a whole number
+    const double a = fmax(((double)z - top) * c, -3000.0);  // below 2^-46; -inf ends there too, also where c is 0
+    const double m = a + 6755399441055744.0, r = a - (m - 6755399441055744.0);
+    const int j = (int)(unsigned)(u64)__double_as_longlong(m);
+    double p = fma(r, 5.732851688640402e-10, 2.1173137155464776e-07);
+    p = fma(r, p, 5.86490495505617e-05);
+    p = fma(r, p, 0.010830424696249145);
+    const double t = table[j & (SAMPLE_EXP - 1)];
+    // the power of two goes to the exponent; adding 2^52 rounds to a whole number in the low bits
+    const double w = __longlong_as_double(__double_as_longlong(fma(t * r, p, t)) + ((long long)(j >> 6) << 52));
+    return (u64)__double_as_longlong(w + 4503599627370496.0) & 0xfffffffffffffULL;
   }
 };
 
-// ONE: the row fits the registers of the workgroup.
-template <typename T, bool ONE>
+// HELD: the row is kept in LDS.
+template <typename T, bool HELD>
 __global__ __launch_bounds__(SAMPLE_THREADS) void sample_kernel(SampleArgs a) {
-  constexpr int VEC = 16 / sizeof(T), U = SAMPLE_PER / VEC;  // logits of a load, loads of a thread and tile
-  __shared__ SampleLds l;
-  const int row = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, V = a.V;
+  constexpr int VEC = 16 / sizeof(T);                        // logits of a chunk
+  using B = Bins<HELD && sizeof(T) == 4 ? 7 : 8>;
+  constexpr int COPIES = HELD && sizeof(T) == 4 ? 1 : 2, OWN = B::BINS / SAMPLE_THREADS;  // bins of a thread
+  constexpr int AHEAD = HELD ? 0 : 2;                        // chunks requested before the one in hand is used
+  __shared__ SampleLds<HELD ? SAMPLE_HELD * (int)sizeof(T) : 0, B::BINS, COPIES> l;
+  const int row = blockIdx.x, tid = threadIdx.x, lane = tid & 63, V = a.V;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const T* zr = (const T*)a.logits + (size_t)row * V;
   const float temp = a.temperature ? a.temperature[row] : 1.f;
   const int top_k = a.top_k ? a.top_k[row] : 0;
   const float top_p = a.top_p ? a.top_p[row] : 1.f;
   const float min_in = a.min_p ? a.min_p[row] : 0.f;
+  const float u_in = a.uniforms[row];
+  asm volatile("" ::: "memory");  // all settings are requested here, before the row
   const u64 least = min_in > 0.f ? (u64)ceil((double)fminf(min_in, 1.f) * 1099511627776.0) : 0;
-  const int n_tiles = ONE ? 1 : (V + SAMPLE_TILE - 1) / SAMPLE_TILE;
-  if (tid < SAMPLE_EXP) l.exp2[tid] = exp2((double)tid * (1.0 / SAMPLE_EXP));
+  const double power = EXP2_TABLE[tid & (SAMPLE_EXP - 1)];
 
-  // ---- the row: element e of load u of a thread is logit tile * TILE + VEC (1024 u + tid) + e
-  float z[SAMPLE_PER];
-  auto load_tile = [&](int tile) {
-    const int base = tile * SAMPLE_TILE + VEC * tid;
-    T raw[U][VEC];
+  // ---- the row.  The waves' runs of `rounds` x 64 chunks follow one another; round u of a lane is the logits
+  // from run + (64 u + lane) VEC on.
+  const int rounds = (V + SAMPLE_THREADS * VEC - 1) / (SAMPLE_THREADS * VEC), length = rounds * 64 * VEC;
+  const int run = wave * length;
+  // Where the largest logit is +inf, those that are share the row: they become 0, all others -inf.
+  bool infinite = false;
+  auto value = [&](float z) {
+    return !infinite ? clean(z) : z == INFINITY ? 0.f : -INFINITY;
+  };
+  auto read = [&](int i, T* c) {  // a chunk; behind the end of the row: -inf
+    if (i + VEC <= V) {
+      __builtin_memcpy(c, zr + i, 16);
+    } else {
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int i = base + VEC * SAMPLE_THREADS * u;
-      if (i + VEC <= V) {
-        __builtin_memcpy(raw[u], zr + i, 16);
-      } else {
-#pragma unroll
-        for (int e = 0; e < VEC; ++e) raw[u][e] = i + e < V ? zr[i + e] : from_f<T>(-INFINITY);
-      }
+      for (int e = 0; e < VEC; ++e) c[e] = i + e < V ? zr[i + e] : from_f<T>(-INFINITY);
     }
-#pragma unroll
-    for (int u = 0; u < U; ++u)
-#pragma unroll
-      for (int e = 0; e < VEC; ++e) z[u * VEC + e] = clean(to_f(raw[u][e]));
   };
-  auto index_of = [&](int tile, int q) { return tile * SAMPLE_TILE + VEC * (SAMPLE_THREADS * (q / VEC) + tid) + q % VEC; };
-  // The logit, as a value that the compiler knows nothing of: what a pass computes from it is not kept in
-  // registers for the next pass, which has no room for it.
-  auto fresh = [&](auto q) {
-    asm volatile("" : "+v"(z[q]));
-    return z[q];
-  };
-  // f(logit, tile, its number in the thread) for every logit of the thread
+  // f(four logits, index of the first) for all of this thread's
   auto each = [&](auto f) {
-    for (int tile = 0; tile < n_tiles; ++tile) {
-      if constexpr (!ONE) load_tile(tile);
-      static_for<0, SAMPLE_PER>([&](auto q) {
-        f(fresh(q), tile, (int)decltype(q)::value);
-        __builtin_amdgcn_sched_barrier(0);
+    T c[AHEAD + 1][VEC];
+    auto get = [&](int u, T* to) {
+      if constexpr (HELD) __builtin_memcpy(to, &l.tile[tid + SAMPLE_THREADS * u], 16);
+      else read(run + (64 * u + lane) * VEC, to);  // one past the last is behind the run, and not used
+    };
+    static_for<0, AHEAD>([&](auto j) { get(j, c[j]); });
+#pragma unroll 1
+    for (int u = 0; u < rounds; ++u) {
+      get(u + AHEAD, c[AHEAD]);
+      static_for<0, VEC / 4>([&](auto g) {
+        constexpr int G = 4 * decltype(g)::value;
+        float v[4] = {clean(to_f(c[0][G])), clean(to_f(c[0][G + 1])), clean(to_f(c[0][G + 2])), clean(to_f(c[0][G + 3]))};
+        if (infinite)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) v[e] = value(v[e]);
+        f(v, run + (64 * u + lane) * VEC + G);
       });
+      static_for<0, AHEAD>([&](auto j) { __builtin_memcpy(c[j], c[j + 1], 16); });
     }
   };
-  if constexpr (ONE) load_tile(0);
+  auto max4 = [](const float* v) { return fmaxf(fmaxf(v[0], v[1]), fmaxf(v[2], v[3])); };
+  auto add_to = [&](int bin, u64 w) { atomicAdd(&l.hist[bin * COPIES + (lane & (COPIES - 1))], w); };
+  auto clear_hist = [&]() {
+#pragma unroll
+    for (int i = 0; i < OWN * COPIES; ++i) l.hist[tid + SAMPLE_THREADS * i] = 0;
+  };
+  if constexpr (HELD) {  // every thread keeps and reads its own chunks
+    constexpr int MOST = SAMPLE_HELD / SAMPLE_THREADS / VEC;
+    T c[MOST][VEC];
+    static_for<0, MOST>([&](auto u) {
+      if ((int)u < rounds) read(run + (64 * (int)u + lane) * VEC, c[u]);
+    });
+    static_for<0, MOST>([&](auto u) {
+      if ((int)u < rounds) __builtin_memcpy(&l.tile[tid + SAMPLE_THREADS * (int)u], c[u], 16);
+    });
+  }
+  if (tid < SAMPLE_EXP) l.exp2[tid] = power;
 
   // ---- the largest logit
   float mine = -INFINITY;
-  each([&](float v, int, int) { mine = fmaxf(mine, v); });
-  float top = mine;
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
+  each([&](const float* v, int) { mine = fmaxf(mine, max4(v)); });
+  float top = row_max(mine);
+  top = fmaxf(fmaxf(lane_of(top, 0), lane_of(top, 16)), fmaxf(lane_of(top, 32), lane_of(top, 48)));
   if (lane == 0) l.redf[wave] = top;
   if (tid == 0) {
     l.n = 0;
     l.at = 0x7fffffff;
   }
-#pragma unroll
-  for (int i = 0; i < SAMPLE_BINS / SAMPLE_THREADS; ++i) l.hist[tid + SAMPLE_THREADS * i] = 0;
+  clear_hist();
+  l.cand[tid] = 0;
   __syncthreads();
-#pragma unroll
-  for (int w = 0; w < SAMPLE_WAVES; ++w) top = fmaxf(top, l.redf[w]);
+  top = lane_of(row_max(l.redf[lane & 15]), 0);
+  if (top == INFINITY) {
+    infinite = true;
+    mine = mine == INFINITY ? 0.f : -INFINITY;
+    top = 0.f;
+  }
   if (top == -INFINITY) {
     if (tid == 0) a.tokens[row] = 0;
     return;
   }
   if (!(temp > 0.f)) {  // the greedy token
     int at = 0x7fffffff;
-    if (mine == top) each([&](float v, int tile, int q) { at = min(at, v == top ? index_of(tile, q) : 0x7fffffff); });
+    if (mine == top)
+      each([&](const float* v, int i) {
+#pragma unroll
+        for (int e = 3; e >= 0; --e) at = v[e] == top ? min(at, i + e) : at;
+      });
     if (at != 0x7fffffff) atomicMin(&l.at, at);
     __syncthreads();
     if (tid == 0) a.tokens[row] = l.at;
     return;
   }
   const unsigned top_key = key_of(top);
-  const Weigh weigh{(double)top, 1.4426950408889634 / (double)temp, l.exp2};
-  const float u_in = a.uniforms[row];
+  const Weigh weigh{(double)top, 92.33248261893306 / (double)temp, l.exp2};
   const double u = u_in > 0.f ? (double)u_in : 0.0;
   auto target_of = [&](u64 total) { return min((u64)fmin(u * (double)total, 9.0e18), total - 1); };
   // the weight that the kept prefix of a total has to reach
@@ -221,256 +303,311 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void sample_kernel(SampleArgs a) {
   // The bin in which the running sum over the bins reaches `want`: l.bin, with what is wanted of it in l.left.
   // False where all bins together do not.
   auto find_bin = [&](u64 want, int turn) {
-    u64 b[4], total;
+    const u64* h = l.hist + OWN * COPIES * tid;
+    u64 b[OWN], sum = 0, total;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) b[i] = l.hist[4 * tid + i];
-    u64 before = block_scan(b[0] + b[1] + b[2] + b[3], l, turn, &total);
+    for (int i = 0; i < OWN; ++i) {
+      b[i] = COPIES == 1 ? h[i] : h[2 * i] + h[2 * i + 1];
+      sum += b[i];
+    }
+    u64 before = block_scan(sum, l, turn, &total);
     if (total < want) return false;  // the same for all threads
+    if (before < want && want <= before + sum) {
+      int bin = OWN * tid;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      if (before < want && want <= before + b[i]) {
-        l.bin = 4 * tid + i;
-        l.left = want - before;
-      }
-      before += b[i];
+      for (int i = 0; i < OWN - 1; ++i)
+        if (want > before + b[i] && bin == OWN * tid + i) {
+          before += b[i];
+          ++bin;
+        }
+      l.bin = bin;
+      l.left = want - before;
     }
     __syncthreads();
     return true;
   };
 
+  // Puts the n tokens of l.cand (zeros behind them) into their order, zeros behind them: a token's place is the
+  // number of larger (key, ~index).
+  auto sort_cand = [&](int n, u64* sorted) {
+    if (tid < n) {
+      const u64 c = l.cand[tid];
+      int place = 0;
+      for (int j0 = 0; j0 < n; j0 += 8) static_for<0, 8>([&](auto j) { place += l.cand[j0 + j] > c; });
+      sorted[place] = c;
+    } else {
+      sorted[tid] = 0;
+    }
+  };
+
   // ---- few of the top: among the tokens that may be
   if (top_k > 0 && top_k <= SAMPLE_THREADS) {
-    if (mine > -INFINITY) atomicAdd(&l.hist[bin_of(top_key - key_of(mine))], (u64)1);
+    if (mine > -INFINITY) add_to(B::of(top_key - key_of(mine)), 1);
     __syncthreads();
-    unsigned low = LOWEST;
-    if (find_bin((u64)top_k, 0)) low = top_key - min(reach_of(l.bin), top_key - LOWEST);
-    const float bound = value_of(low);  // with fewer maxima than k every token
+    float bound = value_of(LOWEST);  // with fewer maxima than k every token
+    if (find_bin((u64)top_k, 0)) bound = value_of(top_key - min(B::last(l.bin), top_key - LOWEST));
     if (mine >= bound)
-      each([&](float v, int tile, int q) {
-        if (v >= bound) {
-          const int at = atomicAdd(&l.n, 1);
-          if (at < SAMPLE_THREADS) l.cand[at] = ((u64)key_of(v) << 32) | (unsigned)~index_of(tile, q);
-        }
+      each([&](const float* v, int i) {
+        if (max4(v) >= bound)
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (v[e] >= bound) {
+              const int at = atomicAdd(&l.n, 1);
+              if (at < SAMPLE_THREADS) l.cand[at] = ((u64)key_of(v[e]) << 32) | (unsigned)~(i + e);
+            }
       });
     __syncthreads();
-    const int n = l.n;
-    if (n <= SAMPLE_THREADS) {
-      // order them: a token's place is the number of larger (key, ~index)
-      u64* const sorted = l.hist;                    // [1024]
-      u64* const weight = l.hist + SAMPLE_THREADS;   // [1024]
-      if (tid < n) {
-        const u64 c = l.cand[tid];
-        int place = 0;
-        for (int j = 0; j < n; ++j) place += l.cand[j] > c;
-        sorted[place] = c;
-      }
-      __syncthreads();
-      const bool in = tid < min(n, top_k);
-      const u64 c = in ? sorted[tid] : 0;
-      u64 w = in ? weigh(value_of((unsigned)(c >> 32))) : 0, total;
-      const u64 before = block_scan(w, l, 1, &total);
-      if (tid > 0 && ((top_p < 1.f && before >= want_of(total)) || w < least)) w = 0;
-      if (in) weight[tid] = w;
-      block_scan(w, l, 0, &total);  // (its barrier: the weights are written)
+    const int n = l.n, m = min(n, top_k);
+    u64* const sorted = l.hist;                   // [1024]
+    u64* const weight = l.hist + SAMPLE_THREADS;  // [1024]
+    // The kept tokens' share of the row: c and w of the token at place `tid` of m, the weight before it, and all.
+    auto cut_weight = [&](u64 w, u64 before, u64 total) {
+      return tid > 0 && ((top_p < 1.f && before >= want_of(total)) || w < least) ? 0 : w;
+    };
+    // Draws among them, once sorted and weight hold them all.
+    auto draw = [&](u64 c, u64 w, u64 total) {
       const u64 target = target_of(total);
-      if (w > 0) {
-        u64 sum = 0;  // of the kept tokens of a lower index
-        const int m = min(n, top_k);
-        for (int j = 0; j < m; ++j) sum += (unsigned)sorted[j] > (unsigned)c ? weight[j] : 0;
-        if (sum <= target && target < sum + w) a.tokens[row] = (int)~(unsigned)c;
-      }
+      u64 sum = 0;  // of the kept tokens of a lower index
+      for (int j0 = 0; j0 < m; j0 += 8)
+        static_for<0, 8>([&](auto j) { sum += (unsigned)sorted[j0 + j] > (unsigned)c ? weight[j0 + j] : 0; });
+      if (w > 0 && sum <= target && target < sum + w) a.tokens[row] = (int)~(unsigned)c;
+    };
+    if (n <= 64) {  // one wave does it, without barriers
+      if (wave > 0) return;
+      sort_cand(n, sorted);
+      __builtin_amdgcn_wave_barrier();
+      const u64 c = sorted[tid];
+      u64 w = tid < m ? weigh(value_of((unsigned)(c >> 32))) : 0;
+      const u64 upto = wave_scan(w);
+      w = cut_weight(w, upto - w, readlane64(upto, 63));
+      weight[tid] = w;
+      __builtin_amdgcn_wave_barrier();
+      draw(c, w, readlane64(wave_scan(w), 63));
+      return;
+    }
+    if (n <= SAMPLE_THREADS) {
+      sort_cand(n, sorted);
+      __syncthreads();
+      const u64 c = sorted[tid];
+      u64 w = tid < m ? weigh(value_of((unsigned)(c >> 32))) : 0, total;
+      const u64 before = block_scan(w, l, 1, &total);
+      w = cut_weight(w, before, total);
+      weight[tid] = w;
+      block_scan(w, l, 0, &total);  // (its barrier: the weights are written)
+      draw(c, w, total);
       return;
     }
     // more equal tokens than places: the long way
     __syncthreads();
-#pragma unroll
-    for (int i = 0; i < SAMPLE_BINS / SAMPLE_THREADS; ++i) l.hist[tid + SAMPLE_THREADS * i] = 0;
+    clear_hist();
     __syncthreads();
   }
 
-  // ---- cuts: kept are the keys above `cut` and the first `ties` tokens of key `cut`
-  unsigned cut = LOWEST - 1;
-  u64 ties = ~0ull;
-  // Moves the cut to where the running sum of `amount` over the tokens above the old cut reaches `want`;
-  // returns what is wanted of the tokens at it.  l.hist holds the first histogram (see bin_of).
-  auto narrow = [&](u64 want, auto amount) {
-    unsigned lo = cut + 1, hi = top_key;
-    int shift = -1;
-    for (;;) {
-      find_bin(want, 0);
-      want = l.left;
-      const int bin = l.bin;
-      auto in_bin = [&](unsigned k) { return (shift < 0 ? bin_of(top_key - k) : (int)((hi - k) >> shift)) == bin; };
-      // the range of the keys in the bin
-      unsigned kl = 0xffffffffu, kh = 0;
-      each([&](float v, int, int) {
-        const unsigned k = key_of(v);
-        if (k >= lo && k <= hi && in_bin(k)) {
-          kl = min(kl, k);
-          kh = max(kh, k);
-        }
-      });
-      if (tid == 0) {
-        l.lo = 0xffffffffu;
-        l.hi = 0;
-      }
-      __syncthreads();  // every thread has read l.bin and its bins
-#pragma unroll
-      for (int i = 0; i < SAMPLE_BINS / SAMPLE_THREADS; ++i) l.hist[tid + SAMPLE_THREADS * i] = 0;
-      if (kh) {
-        atomicMin(&l.lo, kl);
-        atomicMax(&l.hi, kh);
-      }
-      __syncthreads();
-      lo = l.lo;
-      hi = l.hi;
-      if (lo == hi) break;
-      shift = 0;
-      while ((hi - lo) >> shift >= (unsigned)SAMPLE_BINS) ++shift;
-      each([&](float v, int, int) {
-        const unsigned k = key_of(v);
-        if (k >= lo && k <= hi) atomicAdd(&l.hist[(hi - k) >> shift], amount(v));
-      });
-      __syncthreads();
-    }
-    cut = lo;
-    return want;
-  };
-  if (top_k > 0) {
-    each([&](float v, int, int) {
-      if (v > -INFINITY) atomicAdd(&l.hist[bin_of(top_key - key_of(v))], (u64)1);
-    });
-    __syncthreads();
-    u64 valid = 0, b = 0;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) b += l.hist[4 * tid + i];
-    block_scan(b, l, 1, &valid);
-    if ((u64)top_k < valid) {
-      ties = narrow((u64)top_k, [](float) { return (u64)1; });
-    } else {
-      __syncthreads();  // the bins have been read
-#pragma unroll
-      for (int i = 0; i < SAMPLE_BINS / SAMPLE_THREADS; ++i) l.hist[tid + SAMPLE_THREADS * i] = 0;
-      __syncthreads();
-    }
-  }
-  if (top_p < 1.f) {
-    const float cut_v = value_of(cut);
-    u64 sum = 0, tied = 0, above, n_tied;
-    each([&](float v, int, int) {
-      if (v > cut_v) {
-        const u64 w = weigh(v);
-        sum += w;
-        if (w) atomicAdd(&l.hist[bin_of(top_key - key_of(v))], w);
-      }
-      tied += v == cut_v;
-    });
-    block_scan(sum, l, 0, &above);
-    block_scan(tied, l, 1, &n_tied);
-    const u64 at_cut = cut >= LOWEST ? weigh(cut_v) : 0, want = want_of(above + min(ties, n_tied) * at_cut);
-    if (want <= above) {
-      const u64 left = narrow(want, weigh), w = weigh(value_of(cut));
-      ties = (left + w - 1) / w;
-    } else {
-      ties = min(ties, (want - above + at_cut - 1) / at_cut);
-    }
-  }
-
-  // ---- the last index of a token at the cut that is kept
-  const float cut_v = value_of(cut);
-  // Finds the thread's part of a running sum in index order: with amount(value, index), the first index at
-  // which the sum exceeds what target_of_total(total) says (l.at), if it does.
-  auto locate = [&](auto amount, auto target_of_total) {
-    u64 total = 0;
-    int tile = 0;
-    u64 target = 0;
-    if constexpr (!ONE) {
-      for (int t = 0; t < n_tiles; ++t) {
-        load_tile(t);
-        u64 s = 0, all;
-        static_for<0, SAMPLE_PER>([&](auto q) {
-          s += amount(fresh(q), index_of(t, q));
-          __builtin_amdgcn_sched_barrier(0);
-        });
-        block_scan(s, l, t & 1, &all);
-        if (tid == 0) l.tile_total[t] = all;
-        total += all;
-      }
-      __syncthreads();
-      target = target_of_total(total);
-      u64 sum = 0;
-      for (tile = 0; tile < n_tiles - 1; ++tile) {
-        if (target < sum + l.tile_total[tile]) break;
-        sum += l.tile_total[tile];
-      }
-      target -= min(target, sum);
-      load_tile(tile);
-    }
-    // sums of 16 threads and one load: U x 64 of them, in index order
-    u64 part[U];
-    static_for<0, U>([&](auto u_c) {
-      constexpr int Q = decltype(u_c)::value * VEC;
-      u64 s = 0;
-      static_for<Q, Q + VEC>([&](auto q) {
-        s += amount(fresh(q), index_of(tile, q));
-        __builtin_amdgcn_sched_barrier(0);
-      });
-      part[u_c] = s;
-      s = row_scan(s);
-      if ((lane & 15) == 15) l.cand[decltype(u_c)::value * 64 + (tid >> 4)] = s;
-    });
-    __syncthreads();
-    u64 all;
-    const u64 v = tid < U * 64 ? l.cand[tid] : 0;
-    const u64 before = block_scan(v, l, 0, &all);
-    if constexpr (ONE) target = target_of_total(all);
-    if (before <= target && target < before + v) {
-      l.bin = tid;
-      l.left = target - before;
-    }
-    __syncthreads();
-    if (target < all) {
-      const int bin = l.bin;
-      if ((tid >> 4) == (bin & 63)) {
-        u64 left = l.left;
-        static_for<0, U>([&](auto u_c) {
-          constexpr int Q = decltype(u_c)::value * VEC;
-          if ((bin >> 6) != decltype(u_c)::value) return;
-          const u64 s = part[u_c], upto = row_scan(s);
-          if (upto - s <= left && left < upto) {
-            u64 c = upto - s;
-            int at = 0x7fffffff;
-            static_for<Q, Q + VEC>([&](auto q) {
-              c += amount(fresh(q), index_of(tile, q));
-              if (c > left) at = min(at, index_of(tile, q));
-            });
-            l.at = at;
-          }
-        });
-      }
-    }
-    __syncthreads();
-  };
+  // ---- cuts: kept are the tokens above `cut`, and of those equal to it the ones up to index `last` (or,
+  // where `ties` is set, the first `ties` ones: their last index is found further down)
+  float cut = -INFINITY;
   int last = V;
-  if (ties != ~0ull) {
-    // the ties-th token of key `cut` (all of them where there are no more)
-    if (tid == 0) l.at = V;
-    locate([&](float v, int) { return (u64)(v == cut_v); }, [&](u64) { return ties - 1; });
+  u64 ties = 0;
+  // The amount of a token in a cut: its weight (top-p) or 1 (top-k).  One after the other: the cut of top-k, the
+  // cut of top-p, and the draw; one copy of the code for all.
+#pragma unroll 1
+  for (int stage = 0; stage < 3; ++stage) {
+    const bool by_weight = stage > 0, drawing = stage == 2;
+    if (stage == 0 ? top_k <= 0 : stage == 1 && !(top_p < 1.f)) continue;
+    if (!drawing) {
+      // Histograms of the amounts of the tokens with keys lo .. hi: by distance from hi, by Bins (the
+      // first, where these are the tokens above the old cut), or divided by 2^shift.
+      unsigned lo = cut == -INFINITY ? LOWEST : key_of(cut) + 1, hi = top_key;
+      int shift = -1;
+      u64 want = 0;  // the new cut is where their running sum, from the top, reaches this
+      for (;;) {
+        const float from = value_of(lo), upto = value_of(hi);
+        u64 sum = 0, tied = 0;
+        if (shift < 0 && by_weight) {
+          each([&](const float* v, int) {
+            if (!(max4(v) >= from)) return;
+            u64 w[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) w[e] = weigh(v[e]);
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              if (v[e] >= from && w[e]) {
+                sum += w[e];
+                add_to(B::of(top_key - key_of(v[e])), w[e]);
+              }
+          });
+          if (cut > -INFINITY)
+            each([&](const float* v, int i) {
+#pragma unroll
+              for (int e = 0; e < 4; ++e) tied += v[e] == cut && i + e <= last;
+            });
+        } else {
+          each([&](const float* v, int) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              if (v[e] >= from && v[e] <= upto) {
+                const u64 w = by_weight ? weigh(v[e]) : 1;
+                const unsigned d = hi - key_of(v[e]);
+                sum += w;
+                if (w) add_to(shift < 0 ? B::of(d) : (int)(d >> shift), w);
+              }
+          });
+        }
+        if (shift < 0) {
+          u64 above, n_tied;
+          block_scan(sum, l, 0, &above);
+          block_scan(tied, l, 1, &n_tied);
+          const u64 at_cut = by_weight ? weigh(cut) : 0;  // 0 also where nothing was cut
+          want = by_weight ? want_of(above + n_tied * at_cut) : min((u64)top_k, above);
+          if (want > above) {  // among the tokens at the old cut
+            const u64 r = (want - above + at_cut - 1) / at_cut;
+            ties = r < n_tied ? r : 0;
+            break;
+          }
+        } else {
+          __syncthreads();
+        }
+        find_bin(want, 0);
+        want = l.left;
+        // the keys of the bin
+        const unsigned d0 = shift < 0 ? B::first(l.bin) : (unsigned)l.bin << shift;
+        const unsigned d1 = shift < 0 ? B::last(l.bin) : d0 + ((1u << shift) - 1u);
+        const unsigned k1 = hi - d0;  // (no token has the key of -0, but 0 compares equal to it)
+        const float low = value_of(hi - min(d1, hi - lo)), high = value_of(k1 == 0x7fffffffu ? k1 - 1 : k1);
+        if (tid == 0) {
+          l.n = 0;
+          l.lo = 0xffffffffu;
+          l.hi = 0;
+        }
+        l.cand[tid] = 0;
+        __syncthreads();  // and every thread has read its bins
+        clear_hist();
+        // the tokens of the bin: how many, the range of their keys, and themselves if they are few
+        unsigned kl = 0xffffffffu, kh = 0;
+        each([&](const float* v, int i) {
+          if (max4(v) >= low)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              if (v[e] >= low && v[e] <= high) {
+                const unsigned k = key_of(v[e]);
+                kl = min(kl, k);
+                kh = max(kh, k);
+                const int at = atomicAdd(&l.n, 1);
+                if (at < SAMPLE_FEW) l.cand[at] = ((u64)k << 32) | (unsigned)~(i + e);
+              }
+        });
+        if (kh) {
+          atomicMin(&l.lo, kl);
+          atomicMax(&l.hi, kh);
+        }
+        __syncthreads();
+        lo = l.lo;
+        hi = l.hi;
+        const int n = l.n;
+        if (lo == hi) {  // one value
+          cut = value_of(lo);
+          const u64 w = by_weight ? weigh(cut) : 1, r = (want + w - 1) / w;
+          last = V;
+          ties = r < (u64)n ? r : 0;
+          break;
+        }
+        if (n <= SAMPLE_FEW) {
+          u64 *const sorted = l.hist + SAMPLE_THREADS, total;
+          sort_cand(n, sorted);
+          __syncthreads();
+          const u64 c = sorted[tid], w = tid >= n ? 0 : by_weight ? weigh(value_of((unsigned)(c >> 32))) : 1;
+          const u64 before = block_scan(w, l, 1, &total);
+          sorted[tid] = 0;
+          if (before < want && want <= before + w) l.left = c;
+          __syncthreads();
+          cut = value_of((unsigned)(l.left >> 32));
+          last = (int)~(unsigned)l.left;
+          break;
+        }
+        shift = 0;
+        while ((hi - lo) >> shift >= (unsigned)B::BINS) ++shift;
+      }
+      if (!ties) continue;
+    }
+    // Along the indices, over the tokens of at least `least_v`: the first index at which the running sum of the
+    // kept weights exceeds its target (the draw), or of the tokens at the cut the last that is kept.
+    const float least_v = fmaxf(cut, value_of(LOWEST));
+    auto amount = [&](const float* v, int i, u64* w) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) w[e] = weigh(v[e]);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const bool at = v[e] == cut, kept = (v[e] > cut || (at && i + e <= last)) && (w[e] >= least || v[e] == top);
+        w[e] = !drawing ? (u64)at : kept ? w[e] : 0;
+      }
+    };
+    // first the wave's run
+    u64 s = 0, total;
+    if (drawing && last >= V && least == 0) {
+      each([&](const float* v, int) {
+        if (!(max4(v) >= least_v)) return;
+        u64 w[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) w[e] = weigh(v[e]);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) s += v[e] >= least_v ? w[e] : 0;
+      });
+    } else {
+      each([&](const float* v, int i) {
+        if (!(max4(v) >= least_v)) return;
+        u64 w[4];
+        amount(v, i, w);
+        s += (w[0] + w[1]) + (w[2] + w[3]);
+      });
+    }
+    s = wave_scan(s);
+    if (lane == 63) l.part[wave] = s;
+    __syncthreads();
+    if (tid == 0) l.at = V;  // (every thread has read it)
+    const u64 upto = row_scan(l.part[lane & 15]);
+    total = readlane64(upto, 15);
+    u64 target = drawing ? target_of(total) : ties - 1;
+    if (target < total) {
+      int w = 0;
+      u64 base = 0;
+      while (target >= readlane64(upto, w)) base = readlane64(upto, w++);
+      target -= base;
+      // then all threads share the run: `share` logits each, one behind the other
+      const int share = (length + 4 * SAMPLE_THREADS - 1) / (4 * SAMPLE_THREADS) * 4, first = w * length + tid * share;
+      auto four = [&](int i, u64* w4) {
+        float v[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = i + e < V ? value(to_f(zr[i + e])) : -INFINITY;
+        amount(v, i, w4);
+        return (w4[0] + w4[1]) + (w4[2] + w4[3]);
+      };
+      u64 w4[4];
+      s = 0;
+      if (tid * share < length)
+        for (int j = 0; j < share; j += 4) s += four(first + j, w4);
+      u64 before = block_scan(s, l, 0, &total);
+      if (before <= target && target < before + s) {
+        int j = 0;
+        u64 t;
+        while (before + (t = four(first + j, w4)) <= target) {
+          before += t;
+          j += 4;
+        }
+        int e = 0;
+        for (; e < 3 && before + w4[e] <= target; ++e) before += w4[e];
+        l.at = first + j + e;
+      }
+    }
+    __syncthreads();
     last = l.at;
+    ties = 0;
   }
-  // ---- the draw
-  locate(
-      [&](float v, int i) {
-        const u64 w = v > cut_v || (v == cut_v && v > -INFINITY && i <= last) ? weigh(v) : 0;
-        return w >= least || v == top ? w : (u64)0;
-      },
-      [&](u64 total) { return target_of(total); });
-  if (tid == 0) a.tokens[row] = l.at;
+  if (tid == 0) a.tokens[row] = last;
 }
 
 template <typename T>
 static hipError_t sample_launch(const SampleArgs& a, int n_rows, hipStream_t s) {
-  if (a.V <= SAMPLE_TILE)
+  if (a.V <= SAMPLE_HELD)
     hipLaunchKernelGGL((sample_kernel<T, true>), dim3(n_rows), dim3(SAMPLE_THREADS), 0, s, a);
   else
     hipLaunchKernelGGL((sample_kernel<T, false>), dim3(n_rows), dim3(SAMPLE_THREADS), 0, s, a);
