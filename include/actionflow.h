@@ -288,7 +288,8 @@ af_status af_op_lm_head_argmax(af_weights* w, const void* hidden, int32_t M, con
  * 8-bit form: values are e4m3 (4 exponent bits, 3 mantissa bits, largest finite value 448, no
  * infinity), times one fp32 scale for each block of 128 columns, of one row (activations) or of 128
  * rows (weights); where a size is no multiple of 128 the last block holds what is left.  A block of
- * values v is stored with the scale s = max(max |v| / 448, 2^-126) as v / s rounded to nearest even; a
+ * values v is stored with the scale s = max(max |v| / 448, 2^-126) as v / s rounded to nearest even
+ * (the quotient taken in fp32 first, within 2^-22 of itself); a
  * block that holds an infinity or a NaN gets a NaN scale and NaN values throughout. */
 
 /* Residual addition and Norm with an 8-bit result: h = x + resid, rounded to dtype and stored in
@@ -302,7 +303,8 @@ af_status af_op_add_rmsnorm_fp8(int32_t dtype, const void* x, const void* resid,
 
 /* x [M, K] of dtype in the 8-bit form with blocks of block_rows (1 or 128) x 128: q [M, K] e4m3, scales
  * fp32 [ceil(M / block_rows), ceil(K / 128)].  Any M and K >= 1 and any alignment of the element types;
- * more blocks than one launch takes (2^28 of 1 x 128, 2^24 of 128 x 128) are AF_ERR_UNSUPPORTED. */
+ * more blocks than one launch takes (2^28 - 15 of 1 x 128 or more, 2^24 of 128 x 128 or more) are
+ * AF_ERR_UNSUPPORTED. */
 af_status af_op_quantize_fp8(int32_t dtype, const void* x, void* q, float* scales, int32_t M, int32_t K,
                              int32_t block_rows, void* hip_stream);
 
@@ -310,8 +312,10 @@ af_status af_op_quantize_fp8(int32_t dtype, const void* x, void* q, float* scale
  * with blocks of 128 x 128), accumulated in fp32, y of out_dtype (AF_BF16 or AF_F32).  The sums over a
  * block are taken before its scales are applied, and a row's result does not depend on the other rows
  * except through the order of the sum over blocks, which goes by the sizes.
- * Any M and N >= 1.  K % 16 != 0, xq or wq not aligned to 16 bytes, K > 2^22 or more than 2^24 tiles of
- * 16 x 16 results are AF_ERR_UNSUPPORTED. */
+ * A bf16 result comes from 8-bit products, whose own error is 1.4e-5 of a result of like terms; an fp32
+ * result from products that are exact.
+ * Any M and N >= 1.  K % 16 != 0, xq or wq not aligned to 16 bytes, K > 2^22, or 2^23 tiles of 16 x 16
+ * results or more are AF_ERR_UNSUPPORTED. */
 af_status af_op_linear_fp8(const void* xq, const float* xs, const void* wq, const float* ws, void* y,
                            int32_t out_dtype, int32_t M, int32_t N, int32_t K, void* hip_stream);
 

@@ -360,6 +360,8 @@ def _call_on(device: int, stream, fn, *args):
     """Calls the library with GPU ``device`` current, on its current stream unless one is given."""
     if device < 0:
         raise ValueError("tensors must be on a GPU")
+    if stream is not None and stream.device.index != device:
+        raise ValueError(f"tensors are on cuda:{device}, the stream is of {stream.device}")
     if device != torch.cuda.current_device():
         with torch.cuda.device(device):
             return _call_on(device, stream, fn, *args)

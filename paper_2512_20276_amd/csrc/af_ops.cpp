@@ -48,7 +48,7 @@ extern "C" af_status af_op_quantize_fp8(int32_t dtype, const void* x, void* q, f
   if (!aligned(x, dtype_size(dtype)) || !aligned(scales, 4))
     return invalid(me, "a pointer is not aligned to its element type");
   const int64_t blocks = (int64_t)(block_rows == 1 ? M : fp8_blocks(M)) * fp8_blocks(K);
-  const int64_t most = (int64_t)1 << (block_rows == 1 ? 28 : 24);
+  const int64_t most = block_rows == 1 ? (1 << 28) - 15 : 1 << 24;  // 16 blocks, or one, to 256 work-items
   if (blocks >= most) return too_large(me, "blocks", blocks, most);
   AF_HIP(launch_quantize_fp8(dtype, x, q, scales, M, K, block_rows, (hipStream_t)hip_stream));
   return AF_OK;
@@ -69,7 +69,7 @@ extern "C" af_status af_op_linear_fp8(const void* xq, const float* xs, const voi
   }
   const int64_t tiles = (((int64_t)M + 15) / 16) * (((int64_t)N + 15) / 16);
   if (K > FP8_MAX_K) return too_large(me, "columns", K, FP8_MAX_K + 1);
-  if (tiles > 1 << 24) return too_large(me, "tiles of 16 x 16", tiles, (1 << 24) + 1);
+  if (tiles >= 1 << 23) return too_large(me, "tiles of 16 x 16", tiles, 1 << 23);  // of up to 512 work-items each
   const Fp8GemmArgs a{xq, xs, wq, ws, y, M, N, K, fp8_blocks(K)};
   AF_HIP(launch_gemm_fp8(out_dtype, a, (hipStream_t)hip_stream));
   return AF_OK;

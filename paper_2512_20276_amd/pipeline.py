@@ -14,8 +14,8 @@ InPlaceKVShift copy does: stage s always sits in slot s, and after each step the
 copies every live request's keys and values one slot along (af_ring_shift_stages).  The
 attention inputs, and so every output, are the same as with the rotation; only bytes move.
 
-Token feedback stays on the device: the step's greedy tokens are written by the library
-straight into the next step's id buffer.  Stage s of step t feeds stage s+1 of step t+1,
+Token feedback stays on the device: the step's tokens, greedy or (with ``sampling``) drawn
+from the step's logits, are written by the library straight into the next step's id buffer.  Stage s of step t feeds stage s+1 of step t+1,
 and in this row order the stages' tokens (segment order: stage-major) are exactly the next
 step's decode ids: ``out_tokens`` of step t is the slice ids_next[P L_P : P L_P + n_seg];
 the last P entries of a full step are the final tokens of the requests that complete.
@@ -27,7 +27,9 @@ from typing import Callable, Dict, List, Optional
 
 import torch
 
-from . import AF_SEG_EMIT, Ring, Weights, packed_forward, segments_array
+from . import AF_SEG_EMIT, Ring, Weights, op_sample, packed_forward, segments_array
+
+SAMPLING = {"temperature": torch.float32, "top_k": torch.int32, "top_p": torch.float32, "min_p": torch.float32}
 
 
 @dataclass
@@ -48,15 +50,23 @@ class Pipeline:
     first P L_P rows are the embedding-input rows of the step's P prefills (pipeline p's at
     rows [p L_P, (p + 1) L_P)); rows with a token id (instruction tokens, decode rows) are
     ignored.  ``prefill_ids`` is the device int32 [L_P] id pattern of every prefill (-1 for
-    embedding rows)."""
+    embedding rows).
+
+    ``sampling`` (None: greedy tokens) has tokens drawn by ``op_sample``: a dict of its settings
+    (temperature, top_k, top_p, min_p), one number each for all requests.  The random numbers come
+    from a generator of the pipeline's own, seeded with ``sampling_seed``; the last step's are in
+    ``uniforms``, in segment order."""
 
     def __init__(self, weights: Weights, ring: Ring, K: int, prefill_ids: torch.Tensor,
                  prefill_embeds: Callable[[int], torch.Tensor], keep_logits: bool = False,
-                 keep_history: bool = True, stream=None, n_pipes: int = 1, shift: str = "rotate"):
+                 keep_history: bool = True, stream=None, n_pipes: int = 1, shift: str = "rotate",
+                 sampling: Optional[Dict[str, float]] = None, sampling_seed: int = 0):
         if K < 1 or n_pipes < 1:
             raise ValueError("K >= 1 and n_pipes >= 1")
         if shift not in ("rotate", "copy") or (shift == "copy" and (n_pipes != 1 or K < 2)):
             raise ValueError("shift is 'rotate', or 'copy' for one pipeline with K >= 2")
+        if sampling is not None and set(sampling) - set(SAMPLING):
+            raise ValueError(f"sampling takes {', '.join(SAMPLING)}, got {', '.join(sampling)}")
         self.shift = shift
         self.w, self.ring, self.K, self.P = weights, ring, K, n_pipes
         self.L_P = int(prefill_ids.numel())
@@ -72,7 +82,13 @@ class Pipeline:
             b[:P * self.L_P] = prefill_ids.repeat(P)
         self.hidden = torch.empty((self.M_max, D), dtype=weights.dtype, device=dev)
         self.logits = (torch.empty((P * K, weights.shape.vocab), dtype=torch.float32, device=dev)
-                       if keep_logits else None)
+                       if keep_logits or sampling is not None else None)
+        self.sampling = None
+        if sampling is not None:
+            self.sampling = {what: torch.full((P * K,), v, dtype=SAMPLING[what], device=dev) for what, v in sampling.items()}
+            self.uniforms = torch.zeros(P * K, dtype=torch.float32, device=dev)
+            self.generator = torch.Generator(device=dev)
+            self.generator.manual_seed(sampling_seed)
         self.t = 0
         self.counts: Dict[int, int] = {}
         self.history: List[torch.Tensor] = []  # per step: device copy of its tokens
@@ -121,14 +137,20 @@ class Pipeline:
         out_tokens = nxt[base:base + n_seg]
         emb = self.prefill_embeds(t)
         arr = segments_array(segs)
-        packed_forward(self.w, cur[:M], emb[:M], arr, self.ring, self.hidden[:M],
-                       self.logits[:n_seg] if self.keep_logits else None, out_tokens, self.stream)
+        logits = None if self.logits is None else self.logits[:n_seg]
+        packed_forward(self.w, cur[:M], emb[:M], arr, self.ring, self.hidden[:M], logits,
+                       out_tokens if self.sampling is None else None, self.stream)
+        if self.sampling is not None:
+            u = self.uniforms[:n_seg]
+            with torch.cuda.stream(self.stream):
+                u.uniform_(generator=self.generator)
+            op_sample(logits, u, out_tokens, **{what: v[:n_seg] for what, v in self.sampling.items()}, stream=self.stream)
         done = self.finish(segs)
         if self.keep_history:
             self.history.append(out_tokens.clone())
         self.t += 1
         return StepResult(t=t, M=M, segments=[s.astuple() for s in segs], tokens=out_tokens,
-                          hidden=self.hidden[:M], logits=self.logits[:n_seg] if self.keep_logits else None,
+                          hidden=self.hidden[:M], logits=logits if self.keep_logits else None,
                           done=done if self.P > 1 else (done[0] if done else None))
 
     def request_tokens(self, r: int, p: int = 0) -> List[int]:
