@@ -20,15 +20,18 @@
 //    least k tokens reach and hardly more do.  A histogram of the maxima gives it, the tokens past it
 //    (some 50 to 70 for k = 50) meet in LDS, and everything else happens among them.
 //  - otherwise a cut is found by a histogram of counts or weights over the distance from the top, in
-//    bins of 1/128 of that distance (fp32 rows in LDS, where no more bins fit) or 1/256 (256 rows of 131072
-//    bf16 logits, top_p alone: 211 us with 128 bins to an octave, which hold several values of many equal
-//    logits each, 176 with 256); the tokens of the bin that holds it are put into order where they
-//    are few, else the bin is divided again.
+//    bins of 1/128 of that distance (fp32 rows in LDS, where no more bins fit) or 1/256; the tokens of the
+//    bin that holds it are put into order where they are few, else the bin is divided again.
+//  - bf16 logits have few values: the weight of each is computed once into a table in LDS, the cut of top-p
+//    is found by counting values, and the draw adds up weights that it reads, two tokens an instruction
+//    up to there (256 rows of 131072, top_p alone: 177 us with weights computed token by token, 96 so).
 // Bound: with top_k, reading the row and the chain of some ten barriers (64 x 32000 fp32, k = 50: 12.2 us;
-// the read alone is 1.5 us over the whole card, but 64 of 256 CUs have a row); else the 64-bit weights,
-// some 25 instructions a token and pass on the one CU that has the row (64 x 32000 fp32: 15.4 us with
-// temperature alone, 36.5 with top_p; 256 x 131072 bf16: 53.6 and 176).  A row stays on one CU, since
-// sharing it needs a wait between workgroups and these calls come behind a projection that costs more.
+// the read alone is 1.6 us over the whole card, but 64 of 256 CUs have a row); else, for fp32, the 64-bit
+// weights, some 25 instructions a token and pass on the one CU that has the row (64 x 32000: 15.2 us with
+// temperature alone, 36.3 with top_p), for bf16 the passes' accesses to LDS, a token each (256 x 131072:
+// 51 us with temperature alone, of which 32 are two passes that only compare; 96 with top_p).  A row stays
+// on one CU, since sharing it needs a wait between workgroups and these calls come behind a projection that
+// costs more.
 
 #include "af_device.h"
 #include "af_fp8.h"
@@ -39,8 +42,11 @@ constexpr int SAMPLE_THREADS = 1024;
 constexpr int SAMPLE_WAVES = SAMPLE_THREADS / 64;
 constexpr int SAMPLE_HELD = 32768;                        // logits of a row that is kept in LDS
 constexpr int SAMPLE_FEW = 256;                           // tokens of a bin that are put into order
+constexpr int SAMPLE_SPAN = 15 * 128;                     // bf16 magnitudes with a weight in LDS
 constexpr int SAMPLE_EXP = 64;                            // entries of the table of powers of two
 typedef unsigned long long u64;
+typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+typedef short i16x2 __attribute__((ext_vector_type(2)));
 
 // ------------------------------------------------------------------ keys
 // Logits are taken as they come but for NaN (-inf) and -0 (0).  Keys are in their order; a larger logit
@@ -96,12 +102,15 @@ __device__ __forceinline__ u64 readlane64(u64 v, int lane) {
          (unsigned)__builtin_amdgcn_readlane((int)(unsigned)v, lane);
 }
 
-// The row (or nothing) and the histogram, in as many copies, by lane, as there is room for: tokens of a bin
-// that meet in one instruction are added one after the other, and bf16 logits have few values.
-template <int ROW_BYTES, int BINS, int COPIES>
+// The row (or nothing), the histogram, and for bf16 the values' weights and counts, in as many copies, by
+// lane, as there is room for: equal tokens that meet in one instruction are added one after the other.
+template <int ROW_BYTES, int BINS, int SLOTS, int COPIES>
 struct SampleLds {
   uint4 tile[ROW_BYTES / 16 + 1];
-  u64 hist[BINS * COPIES];
+  u64 hist[BINS];
+  u64 table[SLOTS + 1];
+  unsigned count[SLOTS * COPIES + 1];
+  u64 mixed[2];
   u64 cand[SAMPLE_THREADS];
   double exp2[SAMPLE_EXP];
   u64 part[SAMPLE_WAVES], red[2][SAMPLE_WAVES];
@@ -184,10 +193,14 @@ struct Weigh {
 template <typename T, bool HELD>
 __global__ __launch_bounds__(SAMPLE_THREADS) void sample_kernel(SampleArgs a) {
   constexpr int VEC = 16 / sizeof(T);                        // logits of a chunk
-  using B = Bins<HELD && sizeof(T) == 4 ? 7 : 8>;
-  constexpr int COPIES = HELD && sizeof(T) == 4 ? 1 : 2, OWN = B::BINS / SAMPLE_THREADS;  // bins of a thread
+  constexpr bool TABLE = sizeof(T) == 2;
+  using B = Bins<HELD || TABLE ? 7 : 8>;
+  constexpr int OWN = B::BINS / SAMPLE_THREADS;              // bins of a thread
+  constexpr int COPIES = HELD ? 2 : 4;                       // of the counts
+  constexpr int NEAR = SAMPLE_SPAN + 1, FAR = 2 * SAMPLE_SPAN + 2, SLOTS = FAR + 1;
+  constexpr int OWN_S = (SLOTS + SAMPLE_THREADS - 1) / SAMPLE_THREADS;
   constexpr int AHEAD = HELD ? 0 : 2;                        // chunks requested before the one in hand is used
-  __shared__ SampleLds<HELD ? SAMPLE_HELD * (int)sizeof(T) : 0, B::BINS, COPIES> l;
+  __shared__ SampleLds<HELD ? SAMPLE_HELD * (int)sizeof(T) : 0, B::BINS, TABLE ? SLOTS : 0, COPIES> l;
   const int row = blockIdx.x, tid = threadIdx.x, lane = tid & 63, V = a.V;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const T* zr = (const T*)a.logits + (size_t)row * V;
@@ -217,8 +230,8 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void sample_kernel(SampleArgs a) {
       for (int e = 0; e < VEC; ++e) c[e] = i + e < V ? zr[i + e] : from_f<T>(-INFINITY);
     }
   };
-  // f(four logits, index of the first) for all of this thread's
-  auto each = [&](auto f) {
+  // f(chunk, index of its first logit) for all of this thread's
+  auto chunks = [&](auto f) {
     T c[AHEAD + 1][VEC];
     auto get = [&](int u, T* to) {
       if constexpr (HELD) __builtin_memcpy(to, &l.tile[tid + SAMPLE_THREADS * u], 16);
@@ -228,22 +241,28 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void sample_kernel(SampleArgs a) {
 #pragma unroll 1
     for (int u = 0; u < rounds; ++u) {
       get(u + AHEAD, c[AHEAD]);
-      static_for<0, VEC / 4>([&](auto g) {
-        constexpr int G = 4 * decltype(g)::value;
-        float v[4] = {clean(to_f(c[0][G])), clean(to_f(c[0][G + 1])), clean(to_f(c[0][G + 2])), clean(to_f(c[0][G + 3]))};
-        if (infinite)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) v[e] = value(v[e]);
-        f(v, run + (64 * u + lane) * VEC + G);
-      });
+      f(c[0], run + (64 * u + lane) * VEC);
       static_for<0, AHEAD>([&](auto j) { __builtin_memcpy(c[j], c[j + 1], 16); });
     }
   };
+  // f(four logits, index of the first)
+  auto each = [&](auto f) {
+    chunks([&](const T* c, int i) {
+      static_for<0, VEC / 4>([&](auto g) {
+        constexpr int G = 4 * decltype(g)::value;
+        float v[4] = {clean(to_f(c[G])), clean(to_f(c[G + 1])), clean(to_f(c[G + 2])), clean(to_f(c[G + 3]))};
+        if (infinite)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) v[e] = value(v[e]);
+        f(v, i + G);
+      });
+    });
+  };
   auto max4 = [](const float* v) { return fmaxf(fmaxf(v[0], v[1]), fmaxf(v[2], v[3])); };
-  auto add_to = [&](int bin, u64 w) { atomicAdd(&l.hist[bin * COPIES + (lane & (COPIES - 1))], w); };
+  auto add_to = [&](int bin, u64 w) { atomicAdd(&l.hist[bin], w); };
   auto clear_hist = [&]() {
 #pragma unroll
-    for (int i = 0; i < OWN * COPIES; ++i) l.hist[tid + SAMPLE_THREADS * i] = 0;
+    for (int i = 0; i < OWN; ++i) l.hist[tid + SAMPLE_THREADS * i] = 0;
   };
   if constexpr (HELD) {  // every thread keeps and reads its own chunks
     constexpr int MOST = SAMPLE_HELD / SAMPLE_THREADS / VEC;
@@ -259,7 +278,11 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void sample_kernel(SampleArgs a) {
 
   // ---- the largest logit
   float mine = -INFINITY;
-  each([&](const float* v, int) { mine = fmaxf(mine, max4(v)); });
+  chunks([&](const T* c, int) {  // (a maximum drops NaN)
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) mine = fmaxf(mine, to_f(c[e]));
+  });
+  mine = clean(mine);
   float top = row_max(mine);
   top = fmaxf(fmaxf(lane_of(top, 0), lane_of(top, 16)), fmaxf(lane_of(top, 32), lane_of(top, 48)));
   if (lane == 0) l.redf[wave] = top;
@@ -300,23 +323,15 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void sample_kernel(SampleArgs a) {
   auto want_of = [&](u64 total) {
     return max((u64)1, min(total, (u64)ceil((double)fmaxf(top_p, 0.f) * (double)total)));
   };
-  // The bin in which the running sum over the bins reaches `want`: l.bin, with what is wanted of it in l.left.
-  // False where all bins together do not.
-  auto find_bin = [&](u64 want, int turn) {
-    const u64* h = l.hist + OWN * COPIES * tid;
-    u64 b[OWN], sum = 0, total;
-#pragma unroll
-    for (int i = 0; i < OWN; ++i) {
-      b[i] = COPIES == 1 ? h[i] : h[2 * i] + h[2 * i + 1];
-      sum += b[i];
-    }
-    u64 before = block_scan(sum, l, turn, &total);
-    if (total < want) return false;  // the same for all threads
+  // Of this thread's N bins, N tid and so on, with amounts b[] and b's sum `before` them, the one in which the
+  // running sum reaches `want`, if it does: l.bin, with what is wanted of it in l.left.
+  auto reach = [&](auto n_c, const u64* b, u64 sum, u64 before, u64 want) {
+    constexpr int N = decltype(n_c)::value;
     if (before < want && want <= before + sum) {
-      int bin = OWN * tid;
+      int bin = N * tid;
 #pragma unroll
-      for (int i = 0; i < OWN - 1; ++i)
-        if (want > before + b[i] && bin == OWN * tid + i) {
+      for (int i = 0; i < N - 1; ++i)
+        if (want > before + b[i] && bin == N * tid + i) {
           before += b[i];
           ++bin;
         }
@@ -324,6 +339,15 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void sample_kernel(SampleArgs a) {
       l.left = want - before;
     }
     __syncthreads();
+  };
+  // The same over the histogram; false where all bins together do not reach it.
+  auto find_bin = [&](u64 want, int turn) {
+    u64 b[OWN], sum = 0, total;
+#pragma unroll
+    for (int i = 0; i < OWN; ++i) sum += b[i] = l.hist[OWN * tid + i];
+    const u64 before = block_scan(sum, l, turn, &total);
+    if (total < want) return false;  // the same for all threads
+    reach(std::integral_constant<int, OWN>{}, b, sum, before, want);
     return true;
   };
 
@@ -403,6 +427,59 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void sample_kernel(SampleArgs a) {
     __syncthreads();
   }
 
+  // ---- the weights of bf16 values.  A window of 15 octaves of magnitudes, down from that of the largest logit or
+  // of 32 temperatures, has a slot per value, in descending order: SPAN positive ones, slot NEAR for what is nearer
+  // to 0, SPAN negative ones, slot FAR for those of larger magnitude.  So a token's weight is read, not computed, and
+  // the cut of top-p is found by counting.  (Slot 0 is for nothing.)
+  unsigned base = 128;  // the least magnitude inside, in bf16's bits; 0 is never inside
+  const float floor = top - 30.f * temp;  // weights below are 0
+  auto slot_of = [&](float v) {
+    const int bits = (int)__float_as_uint(v), sign = bits >> 31, at = (bits >> 16 & 0x7fff) - (int)base;
+    return (unsigned)at < (unsigned)SAMPLE_SPAN ? NEAR + (at ^ ~sign) - sign : at < 0 ? NEAR : FAR;
+  };
+  auto value_at = [&](int slot) {
+    return __uint_as_float(slot < NEAR ? (base + SAMPLE_SPAN - slot) << 16 : 0x80000000u | (base + slot - NEAR - 1) << 16);
+  };
+  // The slots of two tokens as they are stored; slots 0 and FAR, and SPAN in `at`, for those outside.
+  auto slots_of = [&](u16x2 x, u16x2* at) {
+    const u16x2 sign = (u16x2)((i16x2)x >> (i16x2)15);
+    *at = __builtin_elementwise_min((x & (u16x2)0x7fff) - (u16x2)(unsigned short)base, (u16x2)(unsigned short)SAMPLE_SPAN);
+    return (*at ^ ~sign) - sign + (u16x2)(unsigned short)NEAR;
+  };
+  // f(weight, value) for those tokens of a chunk that are outside, where that is not 0
+  auto outside = [&](const T* c, u16x2 at, auto f) {
+    if (max(at[0], at[1]) < SAMPLE_SPAN) return;
+    u64 w[2];
+    __builtin_memcpy(w, c, 16);
+#pragma unroll 1
+    for (int e = 0; e < VEC; ++e) {  // (one copy of the code)
+      const float v = clean(__uint_as_float((unsigned)w[0] << 16));
+      w[0] = w[0] >> 16 | w[1] << 48;
+      w[1] >>= 16;
+      const int slot = slot_of(v);
+      if ((slot == NEAR || slot == FAR) && v >= floor) f(weigh(v), v);
+    }
+  };
+  if constexpr (TABLE) {
+    const unsigned e = __float_as_uint(fmaxf(fabsf(top), fminf(32.f * temp, 1e38f))) >> 23;
+    base = (e > 15 ? e - 14 : 1) << 7;
+#pragma unroll
+    for (int i = 0; i < OWN_S; ++i) {
+      const int slot = tid + SAMPLE_THREADS * i;
+      if (slot < SLOTS)
+        l.table[slot] = slot == 0 || slot == NEAR || slot == FAR || !(value_at(slot) <= top) ? 0 : weigh(value_at(slot));
+    }
+    for (int i = tid; i < SLOTS * COPIES; i += SAMPLE_THREADS) l.count[i] = 0;
+    if (tid < 2) l.mixed[tid] = 0;
+    __syncthreads();
+  }
+  auto count_of = [&](int slot) {
+    unsigned n = 0;
+#pragma unroll
+    for (int j = 0; j < COPIES; ++j) n += l.count[slot * COPIES + j];
+    return n;
+  };
+
   // ---- cuts: kept are the tokens above `cut`, and of those equal to it the ones up to index `last` (or,
   // where `ties` is set, the first `ties` ones: their last index is found further down)
   float cut = -INFINITY;
@@ -424,6 +501,39 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void sample_kernel(SampleArgs a) {
         const float from = value_of(lo), upto = value_of(hi);
         u64 sum = 0, tied = 0;
         if (shift < 0 && by_weight) {
+          if constexpr (TABLE) {
+            u64 near = 0, far = 0;
+            auto add = [&](u64 w, float v) {
+              if (fabsf(v) < value_at(SAMPLE_SPAN)) near += w;
+              else far += w;
+            };
+            if (cut == -INFINITY && !infinite) {
+              chunks([&](const T* c, int) {
+                u16x2 x[VEC / 2], most = 0, at;
+                __builtin_memcpy(x, c, 16);
+#pragma unroll
+                for (int j = 0; j < VEC / 2; ++j) {
+                  const u16x2 to = slots_of(x[j], &at) * (u16x2)(unsigned short)COPIES + (u16x2)(unsigned short)(lane & (COPIES - 1));
+                  most = __builtin_elementwise_max(most, at);
+                  atomicAdd(&l.count[to[0]], 1u);
+                  atomicAdd(&l.count[to[1]], 1u);
+                }
+                outside(c, most, add);
+              });
+            } else {
+              each([&](const float* v, int) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                  if (!(v[e] >= from)) continue;
+                  const int slot = slot_of(v[e]);
+                  if (slot != NEAR && slot != FAR) atomicAdd(&l.count[slot * COPIES + (lane & (COPIES - 1))], 1u);
+                  else if (v[e] >= floor) add(weigh(v[e]), v[e]);
+                }
+              });
+            }
+            if (near) atomicAdd(&l.mixed[0], near);
+            if (far) atomicAdd(&l.mixed[1], far);
+          } else
           each([&](const float* v, int) {
             if (!(max4(v) >= from)) return;
             u64 w[4];
@@ -453,17 +563,50 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void sample_kernel(SampleArgs a) {
               }
           });
         }
-        if (shift < 0) {
-          u64 above, n_tied;
-          block_scan(sum, l, 0, &above);
+        auto settle = [&](u64 above) {  // false: the cut stays, fewer of the tokens at it are kept
+          u64 n_tied;
           block_scan(tied, l, 1, &n_tied);
           const u64 at_cut = by_weight ? weigh(cut) : 0;  // 0 also where nothing was cut
           want = by_weight ? want_of(above + n_tied * at_cut) : min((u64)top_k, above);
-          if (want > above) {  // among the tokens at the old cut
-            const u64 r = (want - above + at_cut - 1) / at_cut;
-            ties = r < n_tied ? r : 0;
+          if (want <= above) return true;
+          const u64 r = (want - above + at_cut - 1) / at_cut;
+          ties = r < n_tied ? r : 0;
+          return false;
+        };
+        u64 above;
+        if (TABLE && shift < 0 && by_weight) {
+          __syncthreads();
+          u64 b[OWN_S] = {}, all = 0;
+#pragma unroll
+          for (int i = 0; i < OWN_S; ++i) {
+            const int slot = OWN_S * tid + i;
+            if (slot > 0 && slot < SLOTS)
+              b[i] = slot == NEAR ? l.mixed[0] : slot == FAR ? l.mixed[1] : count_of(slot) * l.table[slot];
+            all += b[i];
+          }
+          const u64 before = block_scan(all, l, 0, &above);
+          if (!settle(above)) break;
+          reach(std::integral_constant<int, OWN_S>{}, b, all, before, want);
+          want = l.left;
+          const int slot = l.bin;
+          if (slot != NEAR && slot != FAR) {  // one value
+            cut = value_at(slot);
+            const u64 w = l.table[slot], r = (want + w - 1) / w;
+            last = V;
+            ties = r < (u64)count_of(slot) ? r : 0;
             break;
           }
+          // the keys that share the slot, divided like a bin
+          const float edge = __uint_as_float(slot == FAR ? 0x80000000u | (base + SAMPLE_SPAN) << 16 : (base << 16) - 1u);
+          hi = min(hi, key_of(edge));
+          if (slot == NEAR) lo = max(lo, key_of(-edge));
+          shift = 0;
+          while ((hi - lo) >> shift >= (unsigned)B::BINS) ++shift;
+          continue;
+        }
+        if (shift < 0) {
+          block_scan(sum, l, 0, &above);
+          if (!settle(above)) break;
         } else {
           __syncthreads();
         }
@@ -543,7 +686,39 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void sample_kernel(SampleArgs a) {
     };
     // first the wave's run
     u64 s = 0, total;
-    if (drawing && last >= V && least == 0) {
+    const int cut_slot = TABLE && cut > -INFINITY ? slot_of(cut) : FAR - 1;
+    if (!drawing) {
+      each([&](const float* v, int) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) s += v[e] == cut;
+      });
+    } else if (TABLE && !infinite && cut_slot != NEAR && cut_slot != FAR) {
+      if constexpr (TABLE) {
+        __syncthreads();  // (the table has been read)
+        for (int slot = tid; slot < SLOTS; slot += SAMPLE_THREADS)
+          if (slot > cut_slot || (l.table[slot] < least && value_at(slot) != top)) l.table[slot] = 0;
+        __syncthreads();
+        chunks([&](const T* c, int) {
+          u16x2 x[VEC / 2], most = 0, at;
+          __builtin_memcpy(x, c, 16);
+#pragma unroll
+          for (int j = 0; j < VEC / 2; ++j) {
+            const u16x2 from = slots_of(x[j], &at);
+            most = __builtin_elementwise_max(most, at);
+            s += l.table[from[0]] + l.table[from[1]];
+          }
+          outside(c, most, [&](u64 w, float v) { s += v > cut && (w >= least || v == top) ? w : 0; });
+        });
+        if (last < run + length && cut > -INFINITY) {  // those at the cut that are not kept
+          u64 n = 0;
+          each([&](const float* v, int i) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) n += v[e] == cut && i + e > last;
+          });
+          s -= n * l.table[cut_slot];
+        }
+      }
+    } else if (drawing && last >= V && least == 0) {
       each([&](const float* v, int) {
         if (!(max4(v) >= least_v)) return;
         u64 w[4];

@@ -188,3 +188,37 @@ def test_draws_follow_the_weights():
     assert got == sorted(got)
     n = np.bincount(got, minlength=5)
     assert np.all(np.abs(n - 4096 * np.array([0.1, 0.2, 0.05, 0.4, 0.25])) <= 1.0)
+
+
+# bf16 weights are read from a table of 15 octaves below the larger of the top logit and 32 temperatures
+@pytest.mark.parametrize("V", [777, 5000, 40000])
+@pytest.mark.parametrize("temperature", [0.001, 0.3, 1.0, 50.0, INF])
+@pytest.mark.parametrize("scale,shift", [(1e-38, 0), (1e-4, 0), (1e-2, 0.02), (1.0, 0), (1.0, -100.0), (30.0, 0), (1e4, 0), (1e37, 0)])
+def test_bf16_values_of_any_magnitude(V, temperature, scale, shift):
+    z = (normal((6, V), 31 + V, std=scale) + shift).to(torch.bfloat16)
+    z[1, ::3] = -INF
+    z[2, 1::2] *= 2.0 ** -14
+    z[3, ::2] = z[3, 1]
+    z[4, ::5] = NAN
+    u = uniforms(6, 32 + V)
+    check(z, u, temperature=temperature)
+    check(z, u, temperature=temperature, top_p=[0.99, 0.9, 0.7, 0.5, 0.3, 0.05], min_p=[0, 0, 0, 0.01, 0.5, 0])
+    check(z, u, temperature=temperature, top_k=[1100, 2000, 0, 1300, 1, 1025], top_p=0.8)
+
+
+@pytest.mark.parametrize("V", [3000, 40000])
+def test_bf16_cut_outside_the_table(V):
+    """Most of the weight lies among logits so near to 0, or so far below, that the table has no place for them."""
+    near = normal((8, V), 41, std=2.0 ** -14).to(torch.bfloat16)  # under a top of 1 and 32 temperatures of 32
+    near[:, 17] = 1.0
+    far = (normal((8, V), 42, std=1.5) - 132.0).to(torch.bfloat16)  # |z| >= 128 under a top of -127: past its octave
+    far[:, 23] = -127.0
+    p = [0.01, 0.1, 0.3, 0.5, 0.7, 0.9, 0.99, 0.9999]
+    for z, t in ((near, 1.0), (near, 0.1), (far, 1.0), (far, 0.6)):
+        check(z, uniforms(8, 43), temperature=t, top_p=p)
+        check(z, uniforms(8, 44), temperature=t, top_p=p, min_p=0.0001, top_k=2000)
+    both = torch.where(torch.arange(V, device="cuda") % 2 == 0, near, far)
+    check(both, uniforms(8, 45), temperature=0.3, top_p=p)
+    both[:, 5] = INF
+    both[:, 900::31] = INF
+    check(both, uniforms(8, 46), temperature=0.3, top_p=p)
