@@ -362,7 +362,7 @@ def _call_on(device: int, stream, fn, *args):
         raise ValueError("tensors must be on a GPU")
     if stream is not None and stream.device.index != device:
         raise ValueError(f"tensors are on cuda:{device}, the stream is of {stream.device}")
-    if device != torch.cuda.current_device():
+    if device != torch._C._cuda_getDevice():
         with torch.cuda.device(device):
             return _call_on(device, stream, fn, *args)
     # the raw handle: building a Stream object for it takes as long as the launch

@@ -19,16 +19,18 @@
 //  - top-k of up to 1024: 1024 threads hold a maximum each; the k-th largest of those is a bound that at
 //    least k tokens reach and hardly more do.  A histogram of the maxima gives it, the tokens past it
 //    (some 50 to 70 for k = 50) meet in LDS, and everything else happens among them.
-//  - otherwise a cut is found by a histogram of counts or weights over the distance from the top, in
-//    bins of 1/128 of that distance (fp32 rows in LDS, where no more bins fit) or 1/256; the tokens of the
-//    bin that holds it are put into order where they are few, else the bin is divided again.
+//  - otherwise a cut is found by a histogram: of weights (top-p) over the weight's logarithm, of counts
+//    (top-k) over the distance from the top logit in bins of 1/128 or 1/256 of it; the tokens of the bin that
+//    holds the cut are put into order where they are few, else the bin is divided again.  (Weights over
+//    the distance too met in few bins, where those below 0 are far from any above it: 64 x 32000 fp32
+//    with settings of every kind 47.4 us, so 36.1.)
 //  - bf16 logits have few values: the weight of each is computed once into a table in LDS, the cut of top-p
 //    is found by counting values, and the draw adds up weights that it reads, two tokens an instruction
 //    up to there (256 rows of 131072, top_p alone: 177 us with weights computed token by token, 96 so).
-// Bound: with top_k, reading the row and the chain of some ten barriers (64 x 32000 fp32, k = 50: 12.2 us;
+// Bound: with top_k, reading the row and the chain of some ten barriers (64 x 32000 fp32, k = 50: 12 us;
 // the read alone is 1.6 us over the whole card, but 64 of 256 CUs have a row); else, for fp32, the 64-bit
-// weights, some 25 instructions a token and pass on the one CU that has the row (64 x 32000: 15.2 us with
-// temperature alone, 36.3 with top_p), for bf16 the passes' accesses to LDS, a token each (256 x 131072:
+// weights, some 25 instructions a token and pass on the one CU that has the row (64 x 32000: 14 us with
+// temperature alone, 33 with top_p), for bf16 the passes' accesses to LDS, a token each (256 x 131072:
 // 51 us with temperature alone, of which 32 are two passes that only compare; 96 with top_p).  A row stays
 // on one CU, since sharing it needs a wait between workgroups and these calls come behind a projection that
 // costs more.
@@ -52,7 +54,7 @@ typedef short i16x2 __attribute__((ext_vector_type(2)));
 // Logits are taken as they come but for NaN (-inf) and -0 (0).  Keys are in their order; a larger logit
 // has a larger key, -inf has key LOWEST - 1.
 constexpr unsigned LOWEST = 0x00800000u;
-__device__ __forceinline__ float clean(float z) { return fmaxf(z, -INFINITY) + 0.f; }
+__device__ __forceinline__ float clean(float z) { return fmaxf(z + 0.f, -INFINITY); }
 __device__ __forceinline__ unsigned key_of(float z) {
   const unsigned b = __float_as_uint(z);
   return b ^ ((unsigned)((int)b >> 31) | 0x80000000u);
@@ -175,10 +177,27 @@ __device__ const double EXP2_TABLE[SAMPLE_EXP] = {
 struct Weigh {
   double top, c;
   const double* table;
-  __device__ __forceinline__ u64 operator()(float z) const {
+  // a, with its nearest whole number in the low word of m
+  __device__ __forceinline__ double steps(float z, double* m) const {
     const double a = fmax(((double)z - top) * c, -3000.0);  // below 2^-46; -inf ends there too, also where c is 0
-    const double m = a + 6755399441055744.0, r = a - (m - 6755399441055744.0);
+    *m = a + 6755399441055744.0;
+    return a;
+  }
+  // How many steps of 1/64 of an octave the weight is below the top's: 0 .. 3000, none fewer for a smaller z.
+  __device__ __forceinline__ int below(float z) const {
+    double m;
+    steps(z, &m);
+    return -(int)(unsigned)(u64)__double_as_longlong(m);
+  }
+  __device__ __forceinline__ u64 operator()(float z) const {
+    int j;
+    return at(z, &j);
+  }
+  __device__ __forceinline__ u64 at(float z, int* steps_below) const {
+    double m;
+    const double a = steps(z, &m), r = a - (m - 6755399441055744.0);
     const int j = (int)(unsigned)(u64)__double_as_longlong(m);
+    *steps_below = -j;
     double p = fma(r, 5.732851688640402e-10, 2.1173137155464776e-07);
     p = fma(r, p, 5.86490495505617e-05);
     p = fma(r, p, 0.010830424696249145);
@@ -193,9 +212,10 @@ struct Weigh {
 template <typename T, bool HELD>
 __global__ __launch_bounds__(SAMPLE_THREADS) void sample_kernel(SampleArgs a) {
   constexpr int VEC = 16 / sizeof(T);                        // logits of a chunk
-  constexpr bool TABLE = sizeof(T) == 2;
+  constexpr bool TABLE = sizeof(T) == 2, CLEAN = HELD && !TABLE;  // CLEAN: the row in LDS is clean already
   using B = Bins<HELD || TABLE ? 7 : 8>;
   constexpr int OWN = B::BINS / SAMPLE_THREADS;              // bins of a thread
+  constexpr int STEPS = B::BINS > 3000 ? 0 : 1;              // steps of a bin, as a power of two
   constexpr int COPIES = HELD ? 2 : 4;                       // of the counts
   constexpr int NEAR = SAMPLE_SPAN + 1, FAR = 2 * SAMPLE_SPAN + 2, SLOTS = FAR + 1;
   constexpr int OWN_S = (SLOTS + SAMPLE_THREADS - 1) / SAMPLE_THREADS;
@@ -250,10 +270,14 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void sample_kernel(SampleArgs a) {
     chunks([&](const T* c, int i) {
       static_for<0, VEC / 4>([&](auto g) {
         constexpr int G = 4 * decltype(g)::value;
-        float v[4] = {clean(to_f(c[G])), clean(to_f(c[G + 1])), clean(to_f(c[G + 2])), clean(to_f(c[G + 3]))};
-        if (infinite)
+        float v[4] = {to_f(c[G]), to_f(c[G + 1]), to_f(c[G + 2]), to_f(c[G + 3])};
+        if constexpr (!CLEAN) {
 #pragma unroll
-          for (int e = 0; e < 4; ++e) v[e] = value(v[e]);
+          for (int e = 0; e < 4; ++e) v[e] = clean(v[e]);
+          if (infinite)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] = value(v[e]);
+        }
         f(v, i + G);
       });
     });
@@ -271,7 +295,11 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void sample_kernel(SampleArgs a) {
       if ((int)u < rounds) read(run + (64 * (int)u + lane) * VEC, c[u]);
     });
     static_for<0, MOST>([&](auto u) {
-      if ((int)u < rounds) __builtin_memcpy(&l.tile[tid + SAMPLE_THREADS * (int)u], c[u], 16);
+      if (!((int)u < rounds)) return;
+      if constexpr (CLEAN)
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) c[u][e] = clean(c[u][e]);
+      __builtin_memcpy(&l.tile[tid + SAMPLE_THREADS * (int)u], c[u], 16);
     });
   }
   if (tid < SAMPLE_EXP) l.exp2[tid] = power;
@@ -296,6 +324,12 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void sample_kernel(SampleArgs a) {
   top = lane_of(row_max(l.redf[lane & 15]), 0);
   if (top == INFINITY) {
     infinite = true;
+    if constexpr (CLEAN)
+      for (int u = 0; u < rounds; ++u) {
+        float* c = (float*)&l.tile[tid + SAMPLE_THREADS * u];
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) c[e] = value(c[e]);
+      }
     mine = mine == INFINITY ? 0.f : -INFINITY;
     top = 0.f;
   }
@@ -340,12 +374,16 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void sample_kernel(SampleArgs a) {
     }
     __syncthreads();
   };
-  // The same over the histogram; false where all bins together do not reach it.
-  auto find_bin = [&](u64 want, int turn) {
-    u64 b[OWN], sum = 0, total;
+  auto own_bins = [&](u64* b) {  // of the histogram, and their sum
+    u64 sum = 0;
 #pragma unroll
     for (int i = 0; i < OWN; ++i) sum += b[i] = l.hist[OWN * tid + i];
-    const u64 before = block_scan(sum, l, turn, &total);
+    return sum;
+  };
+  // The same over the histogram; false where all bins together do not reach it.
+  auto find_bin = [&](u64 want, int turn) {
+    u64 b[OWN], total;
+    const u64 sum = own_bins(b), before = block_scan(sum, l, turn, &total);
     if (total < want) return false;  // the same for all threads
     reach(std::integral_constant<int, OWN>{}, b, sum, before, want);
     return true;
@@ -499,7 +537,8 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void sample_kernel(SampleArgs a) {
       u64 want = 0;  // the new cut is where their running sum, from the top, reaches this
       for (;;) {
         const float from = value_of(lo), upto = value_of(hi);
-        u64 sum = 0, tied = 0;
+        const bool steps = !TABLE && shift < 0 && by_weight;  // bins of equal steps of the weight's logarithm
+        u64 tied = 0;
         if (shift < 0 && by_weight) {
           if constexpr (TABLE) {
             u64 near = 0, far = 0;
@@ -535,16 +574,13 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void sample_kernel(SampleArgs a) {
             if (far) atomicAdd(&l.mixed[1], far);
           } else
           each([&](const float* v, int) {
-            if (!(max4(v) >= from)) return;
             u64 w[4];
+            int j[4];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) w[e] = weigh(v[e]);
+            for (int e = 0; e < 4; ++e) w[e] = weigh.at(v[e], &j[e]);
 #pragma unroll
             for (int e = 0; e < 4; ++e)
-              if (v[e] >= from && w[e]) {
-                sum += w[e];
-                add_to(B::of(top_key - key_of(v[e])), w[e]);
-              }
+              if (v[e] >= from && w[e]) add_to(j[e] >> STEPS, w[e]);
           });
           if (cut > -INFINITY)
             each([&](const float* v, int i) {
@@ -558,7 +594,6 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void sample_kernel(SampleArgs a) {
               if (v[e] >= from && v[e] <= upto) {
                 const u64 w = by_weight ? weigh(v[e]) : 1;
                 const unsigned d = hi - key_of(v[e]);
-                sum += w;
                 if (w) add_to(shift < 0 ? B::of(d) : (int)(d >> shift), w);
               }
           });
@@ -604,19 +639,31 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void sample_kernel(SampleArgs a) {
           while ((hi - lo) >> shift >= (unsigned)B::BINS) ++shift;
           continue;
         }
+        __syncthreads();
         if (shift < 0) {
-          block_scan(sum, l, 0, &above);
+          u64 b[OWN];
+          const u64 all = own_bins(b), before = block_scan(all, l, 0, &above);
           if (!settle(above)) break;
+          reach(std::integral_constant<int, OWN>{}, b, all, before, want);
         } else {
-          __syncthreads();
+          find_bin(want, 0);
         }
-        find_bin(want, 0);
         want = l.left;
-        // the keys of the bin
-        const unsigned d0 = shift < 0 ? B::first(l.bin) : (unsigned)l.bin << shift;
-        const unsigned d1 = shift < 0 ? B::last(l.bin) : d0 + ((1u << shift) - 1u);
-        const unsigned k1 = hi - d0;  // (no token has the key of -0, but 0 compares equal to it)
-        const float low = value_of(hi - min(d1, hi - lo)), high = value_of(k1 == 0x7fffffffu ? k1 - 1 : k1);
+        // the values of the bin; of steps: of about it, and then by the steps themselves
+        const int bin = l.bin;
+        float low, high;
+        if (steps) {
+          low = (float)((double)top - (double)(((bin + 1) << STEPS) + 1) / weigh.c);
+          high = (float)((double)top - (double)((bin << STEPS) - 1) / weigh.c);
+          low = fmaxf(low - fabsf(low) * 3e-7f, from);
+          high += fabsf(high) * 3e-7f;
+        } else {
+          const unsigned d0 = shift < 0 ? B::first(bin) : (unsigned)bin << shift;
+          const unsigned d1 = shift < 0 ? B::last(bin) : d0 + ((1u << shift) - 1u);
+          const unsigned k1 = hi - d0;  // (no token has the key of -0, but 0 compares equal to it)
+          low = value_of(hi - min(d1, hi - lo));
+          high = value_of(k1 == 0x7fffffffu ? k1 - 1 : k1);
+        }
         if (tid == 0) {
           l.n = 0;
           l.lo = 0xffffffffu;
@@ -628,16 +675,19 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void sample_kernel(SampleArgs a) {
         // the tokens of the bin: how many, the range of their keys, and themselves if they are few
         unsigned kl = 0xffffffffu, kh = 0;
         each([&](const float* v, int i) {
-          if (max4(v) >= low)
+          bool any = false;
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-              if (v[e] >= low && v[e] <= high) {
-                const unsigned k = key_of(v[e]);
-                kl = min(kl, k);
-                kh = max(kh, k);
-                const int at = atomicAdd(&l.n, 1);
-                if (at < SAMPLE_FEW) l.cand[at] = ((u64)k << 32) | (unsigned)~(i + e);
-              }
+          for (int e = 0; e < 4; ++e) any |= v[e] >= low && v[e] <= high;
+          if (!any) return;
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (v[e] >= low && v[e] <= high && (!steps || weigh.below(v[e]) >> STEPS == bin)) {
+              const unsigned k = key_of(v[e]);
+              kl = min(kl, k);
+              kh = max(kh, k);
+              const int at = atomicAdd(&l.n, 1);
+              if (at < SAMPLE_FEW) l.cand[at] = ((u64)k << 32) | (unsigned)~(i + e);
+            }
         });
         if (kh) {
           atomicMin(&l.lo, kl);
@@ -718,14 +768,21 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void sample_kernel(SampleArgs a) {
           s -= n * l.table[cut_slot];
         }
       }
-    } else if (drawing && last >= V && least == 0) {
+    } else if (least == 0 && cut == -INFINITY) {
       each([&](const float* v, int) {
+        u64 w[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) w[e] = weigh(v[e]);
+        s += (w[0] + w[1]) + (w[2] + w[3]);
+      });
+    } else if (least == 0) {
+      each([&](const float* v, int i) {
         if (!(max4(v) >= least_v)) return;
         u64 w[4];
 #pragma unroll
         for (int e = 0; e < 4; ++e) w[e] = weigh(v[e]);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) s += v[e] >= least_v ? w[e] : 0;
+        for (int e = 0; e < 4; ++e) s += v[e] > cut || (v[e] == cut && i + e <= last) ? w[e] : 0;
       });
     } else {
       each([&](const float* v, int i) {
@@ -752,7 +809,15 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void sample_kernel(SampleArgs a) {
       auto four = [&](int i, u64* w4) {
         float v[4];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = i + e < V ? value(to_f(zr[i + e])) : -INFINITY;
+        for (int e = 0; e < 4; ++e) {
+          if constexpr (HELD) {
+            const int c = (i - w * length) / VEC;
+            v[e] = to_f(((const T*)&l.tile[w * 64 + (c & 63) + SAMPLE_THREADS * (c >> 6)])[i % VEC + e]);
+            if (!CLEAN) v[e] = value(v[e]);
+          } else {
+            v[e] = i + e < V ? value(to_f(zr[i + e])) : -INFINITY;
+          }
+        }
         amount(v, i, w4);
         return (w4[0] + w4[1]) + (w4[2] + w4[3]);
       };
