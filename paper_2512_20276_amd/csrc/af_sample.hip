@@ -26,12 +26,12 @@
 //    with settings of every kind 47.4 us, so 36.1.)
 //  - bf16 logits have few values: the weight of each is computed once into a table in LDS, the cut of top-p
 //    is found by counting values, and the draw adds up weights that it reads, two tokens an instruction
-//    up to there (256 rows of 131072, top_p alone: 177 us with weights computed token by token, 96 so).
+//    up to there (256 rows of 131072, top_p alone: 177 us with weights computed token by token, 82 so).
 // Bound: with top_k, reading the row and the chain of some ten barriers (64 x 32000 fp32, k = 50: 12 us;
 // the read alone is 1.6 us over the whole card, but 64 of 256 CUs have a row); else, for fp32, the 64-bit
 // weights, some 25 instructions a token and pass on the one CU that has the row (64 x 32000: 14 us with
 // temperature alone, 33 with top_p), for bf16 the passes' accesses to LDS, a token each (256 x 131072:
-// 51 us with temperature alone, of which 32 are two passes that only compare; 96 with top_p).  A row stays
+// 43 us with temperature alone, of which 32 are two passes that only compare; 82 with top_p).  A row stays
 // on one CU, since sharing it needs a wait between workgroups and these calls come behind a projection that
 // costs more.
 
@@ -465,8 +465,11 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void sample_kernel(SampleArgs a) {
     __syncthreads();
   }
 
+  float cut = -INFINITY;
+  int last = V;
+  u64 ties = 0;
   // ---- the weights of bf16 values.  A window of 15 octaves of magnitudes, down from that of the largest logit or
-  // of 32 temperatures, has a slot per value, in descending order: SPAN positive ones, slot NEAR for what is nearer
+  // of 16 temperatures, has a slot per value, in descending order: SPAN positive ones, slot NEAR for what is nearer
   // to 0, SPAN negative ones, slot FAR for those of larger magnitude.  So a token's weight is read, not computed, and
   // the cut of top-p is found by counting.  (Slot 0 is for nothing.)
   unsigned base = 128;  // the least magnitude inside, in bf16's bits; 0 is never inside
@@ -484,22 +487,38 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void sample_kernel(SampleArgs a) {
     *at = __builtin_elementwise_min((x & (u16x2)0x7fff) - (u16x2)(unsigned short)base, (u16x2)(unsigned short)SAMPLE_SPAN);
     return (*at ^ ~sign) - sign + (u16x2)(unsigned short)NEAR;
   };
-  // f(weight, value) for those tokens of a chunk that are outside, where that is not 0
-  auto outside = [&](const T* c, u16x2 at, auto f) {
-    if (max(at[0], at[1]) < SAMPLE_SPAN) return;
-    u64 w[2];
-    __builtin_memcpy(w, c, 16);
+  // f(weight, value) for those tokens of a chunk that are outside, where that is not 0; most: the largest `at`
+  auto outside = [&](const T* c, u16x2 most, auto f) {
+    if (max(most[0], most[1]) < SAMPLE_SPAN) return;
+    unsigned x[VEC / 2];
+    __builtin_memcpy(x, c, 16);
+#pragma unroll
+    for (int j = 0; j < VEC / 2; ++j) {
+      u16x2 at;
+      slots_of(__builtin_bit_cast(u16x2, x[j]), &at);
+      if (max(at[0], at[1]) < SAMPLE_SPAN) continue;
 #pragma unroll 1
-    for (int e = 0; e < VEC; ++e) {  // (one copy of the code)
-      const float v = clean(__uint_as_float((unsigned)w[0] << 16));
-      w[0] = w[0] >> 16 | w[1] << 48;
-      w[1] >>= 16;
-      const int slot = slot_of(v);
-      if ((slot == NEAR || slot == FAR) && v >= floor) f(weigh(v), v);
+      for (int e = 0; e < 2; ++e) {
+        const float v = clean(__uint_as_float(e ? x[j] & 0xffff0000u : x[j] << 16));
+        const int slot = slot_of(v);
+        if ((slot == NEAR || slot == FAR) && v >= floor) f(weigh(v), v);
+      }
     }
   };
+  // How many tokens of a chunk from index i on are `cut`, at indices past `after`; of bf16 values other than 0.
+  auto equal = [&](const T* c, int i, int after) {
+    unsigned x[VEC / 2], n = 0;
+    __builtin_memcpy(x, c, 16);
+    const unsigned bits = __float_as_uint(cut);
+#pragma unroll
+    for (int j = 0; j < VEC / 2; ++j) {
+      n += (x[j] << 16) == bits && i + 2 * j > after;
+      n += (x[j] & 0xffff0000u) == bits && i + 2 * j + 1 > after;
+    }
+    return n;
+  };
   if constexpr (TABLE) {
-    const unsigned e = __float_as_uint(fmaxf(fabsf(top), fminf(32.f * temp, 1e38f))) >> 23;
+    const unsigned e = __float_as_uint(fmaxf(fabsf(top), fminf(16.f * temp, 1e38f))) >> 23;
     base = (e > 15 ? e - 14 : 1) << 7;
 #pragma unroll
     for (int i = 0; i < OWN_S; ++i) {
@@ -520,9 +539,6 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void sample_kernel(SampleArgs a) {
 
   // ---- cuts: kept are the tokens above `cut`, and of those equal to it the ones up to index `last` (or,
   // where `ties` is set, the first `ties` ones: their last index is found further down)
-  float cut = -INFINITY;
-  int last = V;
-  u64 ties = 0;
   // The amount of a token in a cut: its weight (top-p) or 1 (top-k).  One after the other: the cut of top-k, the
   // cut of top-p, and the draw; one copy of the code for all.
 #pragma unroll 1
@@ -738,10 +754,15 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void sample_kernel(SampleArgs a) {
     u64 s = 0, total;
     const int cut_slot = TABLE && cut > -INFINITY ? slot_of(cut) : FAR - 1;
     if (!drawing) {
-      each([&](const float* v, int) {
+      unsigned n = 0;
+      if (TABLE && !infinite && cut != 0.f)
+        chunks([&](const T* c, int) { n += equal(c, 0, -1); });
+      else
+        each([&](const float* v, int) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) s += v[e] == cut;
-      });
+          for (int e = 0; e < 4; ++e) n += v[e] == cut;
+        });
+      s = n;
     } else if (TABLE && !infinite && cut_slot != NEAR && cut_slot != FAR) {
       if constexpr (TABLE) {
         __syncthreads();  // (the table has been read)
@@ -760,11 +781,8 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void sample_kernel(SampleArgs a) {
           outside(c, most, [&](u64 w, float v) { s += v > cut && (w >= least || v == top) ? w : 0; });
         });
         if (last < run + length && cut > -INFINITY) {  // those at the cut that are not kept
-          u64 n = 0;
-          each([&](const float* v, int i) {
-#pragma unroll
-            for (int e = 0; e < 4; ++e) n += v[e] == cut && i + e > last;
-          });
+          unsigned n = 0;
+          chunks([&](const T* c, int i) { n += equal(c, i, last); });
           s -= n * l.table[cut_slot];
         }
       }

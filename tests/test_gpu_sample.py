@@ -190,7 +190,7 @@ def test_draws_follow_the_weights():
     assert np.all(np.abs(n - 4096 * np.array([0.1, 0.2, 0.05, 0.4, 0.25])) <= 1.0)
 
 
-# bf16 weights are read from a table of 15 octaves below the larger of the top logit and 32 temperatures
+# bf16 weights are read from a table of 15 octaves below the larger of the top logit and 16 temperatures
 @pytest.mark.parametrize("V", [777, 5000, 40000])
 @pytest.mark.parametrize("temperature", [0.001, 0.3, 1.0, 50.0, INF])
 @pytest.mark.parametrize("scale,shift", [(1e-38, 0), (1e-4, 0), (1e-2, 0.02), (1.0, 0), (1.0, -100.0), (30.0, 0), (1e4, 0), (1e37, 0)])
@@ -209,7 +209,7 @@ def test_bf16_values_of_any_magnitude(V, temperature, scale, shift):
 @pytest.mark.parametrize("V", [3000, 40000])
 def test_bf16_cut_outside_the_table(V):
     """Most of the weight lies among logits so near to 0, or so far below, that the table has no place for them."""
-    near = normal((8, V), 41, std=2.0 ** -14).to(torch.bfloat16)  # under a top of 1 and 32 temperatures of 32
+    near = normal((8, V), 41, std=2.0 ** -14).to(torch.bfloat16)  # under a top of 1 and 16 temperatures of 16
     near[:, 17] = 1.0
     far = (normal((8, V), 42, std=1.5) - 132.0).to(torch.bfloat16)  # |z| >= 128 under a top of -127: past its octave
     far[:, 23] = -127.0
