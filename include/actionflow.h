@@ -283,7 +283,8 @@ af_status af_op_lm_head_argmax(af_weights* w, const void* hidden, int32_t M, con
  * Operators next to the single steps above, for programs that keep projection weights in 8 bits or
  * answer with drawn instead of greedy tokens.  Not steps of the paper's method.  None of them
  * allocates, waits or keeps anything between calls, so they run on any stream, on several at once, and
- * under graph capture; tensors are dense and row-major, and every pointer is a device pointer.
+ * under graph capture; tensors are dense and row-major, every pointer is a device pointer, and what is
+ * written overlaps nothing else unless said so.
  *
  * 8-bit form: values are e4m3 (4 exponent bits, 3 mantissa bits, largest finite value 448, no
  * infinity), times one fp32 scale for each block of 128 columns, of one row (activations) or of 128

@@ -26,12 +26,12 @@
 //    with settings of every kind 47.4 us, so 36.1.)
 //  - bf16 logits have few values: the weight of each is computed once into a table in LDS, the cut of top-p
 //    is found by counting values, and the draw adds up weights that it reads, two tokens an instruction
-//    up to there (256 rows of 131072, top_p alone: 177 us with weights computed token by token, 82 so).
+//    up to there (256 rows of 131072, top_p alone: 177 us with weights computed token by token, 66 so).
 // Bound: with top_k, reading the row and the chain of some ten barriers (64 x 32000 fp32, k = 50: 12 us;
 // the read alone is 1.6 us over the whole card, but 64 of 256 CUs have a row); else, for fp32, the 64-bit
 // weights, some 25 instructions a token and pass on the one CU that has the row (64 x 32000: 14 us with
 // temperature alone, 33 with top_p), for bf16 the passes' accesses to LDS, a token each (256 x 131072:
-// 43 us with temperature alone, of which 32 are two passes that only compare; 82 with top_p).  A row stays
+// 43 us with temperature alone, of which 32 are two passes that only compare; 66 with top_p).  A row stays
 // on one CU, since sharing it needs a wait between workgroups and these calls come behind a projection that
 // costs more.
 
@@ -507,7 +507,7 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void sample_kernel(SampleArgs a) {
   };
   // How many tokens of a chunk from index i on are `cut`, at indices past `after`; of bf16 values other than 0.
   auto equal = [&](const T* c, int i, int after) {
-    unsigned x[VEC / 2], n = 0;
+    unsigned x[4], n = 0;
     __builtin_memcpy(x, c, 16);
     const unsigned bits = __float_as_uint(cut);
 #pragma unroll
@@ -539,6 +539,11 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void sample_kernel(SampleArgs a) {
 
   // ---- cuts: kept are the tokens above `cut`, and of those equal to it the ones up to index `last` (or,
   // where `ties` is set, the first `ties` ones: their last index is found further down)
+  // Whether the draw can read its weights: the cut has a slot of its own, or there is none.
+  auto by_slot = [&]() {
+    const int slot = cut > -INFINITY ? slot_of(cut) : FAR - 1;
+    return TABLE && !infinite && slot != NEAR && slot != FAR;
+  };
   // The amount of a token in a cut: its weight (top-p) or 1 (top-k).  One after the other: the cut of top-k, the
   // cut of top-p, and the draw; one copy of the code for all.
 #pragma unroll 1
@@ -736,25 +741,24 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void sample_kernel(SampleArgs a) {
         shift = 0;
         while ((hi - lo) >> shift >= (unsigned)B::BINS) ++shift;
       }
-      if (!ties) continue;
+      if (!ties || (stage == 1 && by_slot())) continue;  // (by slots, the draw finds the last one itself)
     }
     // Along the indices, over the tokens of at least `least_v`: the first index at which the running sum of the
     // kept weights exceeds its target (the draw), or of the tokens at the cut the last that is kept.
     const float least_v = fmaxf(cut, value_of(LOWEST));
-    auto amount = [&](const float* v, int i, u64* w) {
+    auto amount = [&](const float* v, int i, bool counting, u64* w) {
 #pragma unroll
       for (int e = 0; e < 4; ++e) w[e] = weigh(v[e]);
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         const bool at = v[e] == cut, kept = (v[e] > cut || (at && i + e <= last)) && (w[e] >= least || v[e] == top);
-        w[e] = !drawing ? (u64)at : kept ? w[e] : 0;
+        w[e] = counting ? (u64)at : kept ? w[e] : 0;
       }
     };
-    // first the wave's run
-    u64 s = 0, total;
-    const int cut_slot = TABLE && cut > -INFINITY ? slot_of(cut) : FAR - 1;
+    // first the wave's run: s, and with `ties` in a draw the number of its tokens at the cut
+    u64 s = 0, total, w_cut = 0;
+    unsigned n = 0;
     if (!drawing) {
-      unsigned n = 0;
       if (TABLE && !infinite && cut != 0.f)
         chunks([&](const T* c, int) { n += equal(c, 0, -1); });
       else
@@ -763,13 +767,15 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void sample_kernel(SampleArgs a) {
           for (int e = 0; e < 4; ++e) n += v[e] == cut;
         });
       s = n;
-    } else if (TABLE && !infinite && cut_slot != NEAR && cut_slot != FAR) {
+    } else if (by_slot()) {
       if constexpr (TABLE) {
+        const int cut_slot = cut > -INFINITY ? slot_of(cut) : FAR;
+        if (ties) w_cut = l.table[cut_slot] < least && cut != top ? 0 : l.table[cut_slot];
         __syncthreads();  // (the table has been read)
         for (int slot = tid; slot < SLOTS; slot += SAMPLE_THREADS)
-          if (slot > cut_slot || (l.table[slot] < least && value_at(slot) != top)) l.table[slot] = 0;
+          if (slot + (ties > 0) > cut_slot || (l.table[slot] < least && value_at(slot) != top)) l.table[slot] = 0;
         __syncthreads();
-        chunks([&](const T* c, int) {
+        chunks([&](const T* c, int i) {
           u16x2 x[VEC / 2], most = 0, at;
           __builtin_memcpy(x, c, 16);
 #pragma unroll
@@ -778,10 +784,10 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void sample_kernel(SampleArgs a) {
             most = __builtin_elementwise_max(most, at);
             s += l.table[from[0]] + l.table[from[1]];
           }
+          if (ties) n += equal(c, i, -1);
           outside(c, most, [&](u64 w, float v) { s += v > cut && (w >= least || v == top) ? w : 0; });
         });
-        if (last < run + length && cut > -INFINITY) {  // those at the cut that are not kept
-          unsigned n = 0;
+        if (!ties && last < run + length && cut > -INFINITY) {  // those at the cut that are not kept
           chunks([&](const T* c, int i) { n += equal(c, i, last); });
           s -= n * l.table[cut_slot];
         }
@@ -806,15 +812,23 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void sample_kernel(SampleArgs a) {
       each([&](const float* v, int i) {
         if (!(max4(v) >= least_v)) return;
         u64 w[4];
-        amount(v, i, w);
+        amount(v, i, false, w);
         s += (w[0] + w[1]) + (w[2] + w[3]);
       });
     }
+    const bool open = drawing && ties > 0;  // the last token at the cut that is kept has to be found
     s = wave_scan(s);
-    if (lane == 63) l.part[wave] = s;
+    const u64 at_cut = open ? wave_scan(n) : 0;
+    if (lane == 63) {
+      l.part[wave] = s;
+      l.cand[wave] = at_cut;
+    }
     __syncthreads();
     if (tid == 0) l.at = V;  // (every thread has read it)
-    const u64 upto = row_scan(l.part[lane & 15]);
+    u64 run_weight = l.part[lane & 15];
+    const u64 run_n = l.cand[lane & 15], before_n = row_scan(run_n) - run_n;
+    if (open) run_weight += min(run_n, max(ties, before_n) - before_n) * w_cut;
+    const u64 upto = row_scan(run_weight);
     total = readlane64(upto, 15);
     u64 target = drawing ? target_of(total) : ties - 1;
     if (target < total) {
@@ -824,6 +838,7 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void sample_kernel(SampleArgs a) {
       target -= base;
       // then all threads share the run: `share` logits each, one behind the other
       const int share = (length + 4 * SAMPLE_THREADS - 1) / (4 * SAMPLE_THREADS) * 4, first = w * length + tid * share;
+      bool counting = !drawing;
       auto four = [&](int i, u64* w4) {
         float v[4];
 #pragma unroll
@@ -836,24 +851,40 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void sample_kernel(SampleArgs a) {
             v[e] = i + e < V ? value(to_f(zr[i + e])) : -INFINITY;
           }
         }
-        amount(v, i, w4);
+        amount(v, i, counting, w4);
         return (w4[0] + w4[1]) + (w4[2] + w4[3]);
       };
-      u64 w4[4];
-      s = 0;
-      if (tid * share < length)
-        for (int j = 0; j < share; j += 4) s += four(first + j, w4);
-      u64 before = block_scan(s, l, 0, &total);
-      if (before <= target && target < before + s) {
-        int j = 0;
-        u64 t;
-        while (before + (t = four(first + j, w4)) <= target) {
-          before += t;
-          j += 4;
+      u64 w4[4], goal = target;
+      if (open) {  // is the last kept one in this run?
+        const u64 n0 = readlane64(before_n, w), n1 = n0 + readlane64(run_n, w);
+        last = ties >= n1 ? V : -1;
+        if (ties > n0 && ties < n1) {
+          counting = true;
+          goal = ties - 1 - n0;
         }
-        int e = 0;
-        for (; e < 3 && before + w4[e] <= target; ++e) before += w4[e];
-        l.at = first + j + e;
+      }
+#pragma unroll 1
+      for (;;) {
+        s = 0;
+        if (tid * share < length)
+          for (int j = 0; j < share; j += 4) s += four(first + j, w4);
+        u64 before = block_scan(s, l, counting, &total);
+        if (before <= goal && goal < before + s) {
+          int j = 0;
+          u64 t;
+          while (before + (t = four(first + j, w4)) <= goal) {
+            before += t;
+            j += 4;
+          }
+          int e = 0;
+          for (; e < 3 && before + w4[e] <= goal; ++e) before += w4[e];
+          l.at = first + j + e;
+        }
+        if (!drawing || !counting) break;
+        __syncthreads();
+        last = l.at;  // then the draw
+        counting = false;
+        goal = target;
       }
     }
     __syncthreads();

@@ -222,3 +222,18 @@ def test_bf16_cut_outside_the_table(V):
     both[:, 5] = INF
     both[:, 900::31] = INF
     check(both, uniforms(8, 46), temperature=0.3, top_p=p)
+
+
+@pytest.mark.parametrize("V", [130, 5000, 40000, 140000])
+@pytest.mark.parametrize("min_p", [0.0, 0.2])
+def test_bf16_few_values_cut_anywhere(V, min_p):
+    """The cut splits tokens of one value, wherever that is in the row, and the draw falls before, in and behind it."""
+    n = 32
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(V)
+    z = torch.randint(1, 5, (n, V), generator=gen, device="cuda").to(torch.bfloat16)
+    z[: n // 2, V // 3:] = 1.0  # nearly all the equal ones at the end
+    z[n // 2: n // 2 + 4, : V // 2] = 2.0
+    p = torch.linspace(0.02, 0.98, n)
+    check(z, uniforms(n, V + 1), top_p=p.tolist(), min_p=min_p)
+    check(z, 0.97, top_p=p.tolist(), min_p=min_p, temperature=2.0)
