@@ -551,8 +551,9 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void sample_kernel(SampleArgs a) {
     const bool by_weight = stage > 0, drawing = stage == 2;
     if (stage == 0 ? top_k <= 0 : stage == 1 && !(top_p < 1.f)) continue;
     if (!drawing) {
-      // Histograms of the amounts of the tokens with keys lo .. hi: by distance from hi, by Bins (the
-      // first, where these are the tokens above the old cut), or divided by 2^shift.
+      // Histograms of the amounts of the tokens with keys lo .. hi.  The first is of all above the old cut: of counts
+      // by Bins of the distance from hi, of weights by steps of their logarithm, or of bf16 values one by one.  Then
+      // the bin that holds the new cut, in parts of 2^shift keys.
       unsigned lo = cut == -INFINITY ? LOWEST : key_of(cut) + 1, hi = top_key;
       int shift = -1;
       u64 want = 0;  // the new cut is where their running sum, from the top, reaches this
@@ -593,16 +594,17 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void sample_kernel(SampleArgs a) {
             }
             if (near) atomicAdd(&l.mixed[0], near);
             if (far) atomicAdd(&l.mixed[1], far);
-          } else
-          each([&](const float* v, int) {
-            u64 w[4];
-            int j[4];
+          } else {
+            each([&](const float* v, int) {
+              u64 w[4];
+              int j[4];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) w[e] = weigh.at(v[e], &j[e]);
+              for (int e = 0; e < 4; ++e) w[e] = weigh.at(v[e], &j[e]);
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-              if (v[e] >= from && w[e]) add_to(j[e] >> STEPS, w[e]);
-          });
+              for (int e = 0; e < 4; ++e)
+                if (v[e] >= from && w[e]) add_to(j[e] >> STEPS, w[e]);
+            });
+          }
           if (cut > -INFINITY)
             each([&](const float* v, int i) {
 #pragma unroll
