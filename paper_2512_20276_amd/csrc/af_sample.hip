@@ -11,7 +11,7 @@
 // is off by more than the share of most of them).  Tokens below 2^-41 of the top one weigh nothing.
 //
 // One workgroup of 1024 threads per row, which keeps a row of up to 32768 logits in LDS, so that memory
-// is read once (longer ones are read again in every pass, 48 KB of a row under way at a time).  Passes are
+// is read once (longer ones are read again in every pass, 32 to 48 KB of a row under way at a time).  Passes are
 // loops over chunks of 16 bytes a thread: with the row in registers they were unrolled 32 times, and
 // fetching those instructions took longer than executing them (64 rows of 32000 fp32 logits, top_p alone:
 // 45.6 us, as loops 36.5).
@@ -26,12 +26,12 @@
 //    with settings of every kind 47.4 us, so 36.1.)
 //  - bf16 logits have few values: the weight of each is computed once into a table in LDS, the cut of top-p
 //    is found by counting values, and the draw adds up weights that it reads, two tokens an instruction
-//    up to there (256 rows of 131072, top_p alone: 177 us with weights computed token by token, 66 so).
+//    up to there (256 rows of 131072, top_p alone: 177 us with weights computed token by token, 65 so).
 // Bound: with top_k, reading the row and the chain of some ten barriers (64 x 32000 fp32, k = 50: 12 us;
 // the read alone is 1.6 us over the whole card, but 64 of 256 CUs have a row); else, for fp32, the 64-bit
 // weights, some 25 instructions a token and pass on the one CU that has the row (64 x 32000: 14 us with
 // temperature alone, 33 with top_p), for bf16 the passes' accesses to LDS, a token each (256 x 131072:
-// 43 us with temperature alone, of which 32 are two passes that only compare; 66 with top_p).  A row stays
+// 41 us with temperature alone, of which 30 are two passes that only compare; 65 with top_p).  A row stays
 // on one CU, since sharing it needs a wait between workgroups and these calls come behind a projection that
 // costs more.
 
@@ -219,7 +219,9 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void sample_kernel(SampleArgs a) {
   constexpr int COPIES = HELD ? 2 : 4;                       // of the counts
   constexpr int NEAR = SAMPLE_SPAN + 1, FAR = 2 * SAMPLE_SPAN + 2, SLOTS = FAR + 1;
   constexpr int OWN_S = (SLOTS + SAMPLE_THREADS - 1) / SAMPLE_THREADS;
-  constexpr int AHEAD = HELD ? 0 : 2;                        // chunks requested before the one in hand is used
+  // chunks requested before the one in hand is used (131072 logits, k = 50: fp32 23.3 us with one, 19.5 with two, 20.8 with
+  // four; bf16 29.9, 31.7 and, with spilt registers, 34.2)
+  constexpr int AHEAD = HELD ? 0 : TABLE ? 1 : 2;
   __shared__ SampleLds<HELD ? SAMPLE_HELD * (int)sizeof(T) : 0, B::BINS, TABLE ? SLOTS : 0, COPIES> l;
   const int row = blockIdx.x, tid = threadIdx.x, lane = tid & 63, V = a.V;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
