@@ -214,7 +214,7 @@ static void stream_launch(const Fp8GemmArgs& a, hipStream_t s) {
 // stages of 40 KB as with seven of 20 KB, its products alone 27.2), so its time goes by the bytes of a
 // workgroup, (BM + BN) K.  Operands loaded straight to registers came at half that rate (55.6 us: an access
 // of 16 rows x 64 bytes takes half lines).  Large tiles are bound by the matrix cores and the scaling of
-// their results, four fma a product: 2264 x 22016 x 4096 at 1.9 PFLOP/s, the matrix cores busy half the time.
+// their results, four fma a product: 2264 x 22016 x 4096 at 2.0 PFLOP/s, the matrix cores busy half the time.
 //
 // The rows' scales come eight blocks at a time, 16 bytes a load (loaded block by block each was a request
 // of its own for 4 bytes: a third of all requests to L2), through registers into LDS, turned to [block][row].
@@ -478,15 +478,16 @@ static void tile_launch(const Fp8GemmArgs& a, hipStream_t s) {
 // whole), stages of its K loop in each of them, and the stages and results of the whole work where
 // the GPU is busy (in units of a full pass: L2 and HBM then set the pace of a stage).  Coefficients are a
 // least-squares fit to 21 row counts (1..2264) of 10 weight shapes (512 x 4096 .. 32000 x 4096, K 512 ..
-// 11008): the variant of the least estimate takes 1.5 % longer than the fastest one timed on the mean (bf16
-// results; fp32 1.8 %), 22 % at the worst.  Measured, us, against the next variants:
+// 11008), for fp32 results also to 10 of 5 shapes with K 64 .. 256.  The variant of the least estimate takes
+// 1.5 % longer than the fastest one timed on the mean (fp32 0.7 %), 24 % at the worst; with K of 256 and
+// less, where a call takes 3 to 20 us, 7 % (fp32 2 %).  Measured, us, against the next variants:
 //   rows x columns x K       taken                      others
-//   7 x 32000 x 4096         16 x 32 streamed 26.3      16 x 16 streamed 32, 64 x 64 29
-//   64 x 4096 x 4096         32 x 32, four groups 10.3  64 x 64 12.4
-//   282 x 4096 x 11008       96 x 64, two groups 33.1   64 x 64 39.6, 160 x 128 58.5
-//   282 x 22016 x 4096       160 x 256 55.3             256 x 256 59.7, 128 x 256 60.8
-//   1000 x 4096 x 4096       128 x 128, two groups 25.7 160 x 128 26.9, 128 x 256 32.8
-//   2264 x 22016 x 4096      288 x 256 212              256 x 256 237, 128 x 256 248
+//   7 x 32000 x 4096         16 x 32 streamed 25.7      64 x 64 27.0, 16 x 16 streamed 30.5
+//   64 x 4096 x 4096         32 x 32, four groups 10.4  32 x 64 11.7, 64 x 64 13.4
+//   282 x 4096 x 11008       96 x 64, two groups 32.9   64 x 64 40.1, 128 x 128 52.6
+//   282 x 22016 x 4096       160 x 256 53.9             256 x 256 54.5, 128 x 256 60.3
+//   1024 x 4096 x 4096       128 x 128, two groups 25.4 160 x 128 26.8, 128 x 256 31.3
+//   2264 x 22016 x 4096      288 x 256 219              256 x 256 226, 128 x 256 237
 // The streamed ones (K split over the waves, operands straight to registers) are for up to 32 rows: past
 // that they read the activations again for every 16 or 32 columns.
 struct Fp8Variant {
@@ -514,18 +515,18 @@ static const Fp8Variant BF16_VARIANTS[] = {
 // fp32 results: the operands widened to bf16, so twice the time in the matrix cores and more registers
 // (the two largest tiles would not fit them)
 static const Fp8Variant F32_VARIANTS[] = {
-    {16, 16, 8, 512, true, 2.12f, 0.00f, 0.52f, 1.11f, 0.00f},
-    {16, 32, 8, 512, true, 0.00f, 2.12f, 1.00f, 1.44f, 0.00f},
-    {32, 16, 8, 512, true, 0.00f, 2.39f, 0.79f, 0.70f, 0.04f},
-    {32, 32, 4, 256, false, 1.33f, 1.89f, 0.63f, 0.18f, 0.50f},
-    {64, 64, 2, 256, false, 1.66f, 1.90f, 0.73f, 0.09f, 1.57f},
-    {64, 64, 2, 512, false, 3.06f, 0.00f, 0.80f, 0.62f, 4.16f},
-    {32, 64, 4, 256, false, 1.57f, 2.75f, 0.88f, 0.35f, 0.37f},
-    {96, 64, 2, 256, false, 1.71f, 2.12f, 0.95f, 0.09f, 2.14f},
-    {128, 128, 2, 256, false, 3.55f, 1.42f, 1.70f, 0.18f, 6.93f},
-    {160, 128, 2, 256, false, 3.87f, 1.64f, 1.98f, 0.11f, 7.58f},
-    {128, 256, 1, 256, false, 5.56f, 0.00f, 1.49f, 0.00f, 15.29f},
-    {160, 256, 1, 256, false, 5.62f, 0.00f, 1.81f, 0.00f, 17.10f},
+    {16, 16, 8, 512, true, 1.70f, 0.00f, 0.82f, 0.50f, 0.00f},
+    {16, 32, 8, 512, true, 1.49f, 0.00f, 1.34f, 0.70f, 0.00f},
+    {32, 16, 8, 512, true, 0.00f, 2.14f, 1.06f, 0.00f, 0.00f},
+    {32, 32, 4, 256, false, 1.33f, 1.71f, 0.67f, 0.22f, 0.00f},
+    {64, 64, 2, 256, false, 1.09f, 2.22f, 0.72f, 0.12f, 0.25f},
+    {64, 64, 2, 512, false, 2.09f, 0.64f, 0.82f, 0.67f, 2.01f},
+    {32, 64, 4, 256, false, 1.19f, 2.85f, 0.92f, 0.34f, 0.00f},
+    {96, 64, 2, 256, false, 1.02f, 2.53f, 0.89f, 0.16f, 0.38f},
+    {128, 128, 2, 256, false, 1.19f, 3.43f, 1.63f, 0.37f, 1.82f},
+    {160, 128, 2, 256, false, 1.13f, 3.79f, 2.00f, 0.34f, 2.30f},
+    {128, 256, 1, 256, false, 1.02f, 3.30f, 1.51f, 0.26f, 4.18f},
+    {160, 256, 1, 256, false, 1.61f, 2.89f, 1.75f, 0.37f, 4.85f},
 };
 
 int gemm_fp8_plan(int out_dtype, int M, int N, int K) {
