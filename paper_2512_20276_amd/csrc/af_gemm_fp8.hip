@@ -433,12 +433,15 @@ __global__ __launch_bounds__(64 * WM * WN * KG, 1) void gemm_fp8_tile_kernel(Fp8
   } else {
     // A lane's four results of a row are a quarter or half of a line.  So the results of 16 rows are turned in LDS of
     // the wave's own, and a store takes rows of 16 CN columns: whole lines where CN = 4 (2264 x 22016 x 4096:
-    // 205 us, four results a store 219; 208 x 22016 x 128 to fp32: 8.3 and 14.2).
+    // 205 us, four results a store 219; 208 x 22016 x 128 to fp32: 8.4 and 14.2).
     constexpr int PER = 16 / sizeof(O), ROW = 16 * CN, PITCH = ROW + PER;  // of a 16-byte piece, a row, and padded
     constexpr int PIECES = ROW / PER;
     static_assert(S::RED + WM * WN * 16 * PITCH * (int)sizeof(O) <= (int)sizeof(smem), "LDS");
     O* const turn = (O*)(smem + S::RED) + (wn * WM + wm) * (16 * PITCH);  // behind the sums that others still read
     const int n0w = n0 + wn * ROW;
+    // Past L2 where the pieces are aligned: no line of the results is read before the next launch, which does not
+    // find it in L2 (282 x 22016 x 4096 50.9 us, through L2 51.6; 208 x 22016 x 128 to fp32 7.0 and 8.4).
+    const bool aligned = a.N % PER == 0 && (uintptr_t)a.y % 16 == 0;
     static_for<0, RM>([&](auto i) {
       static_for<0, CN>([&](auto j) {
         const float r[4] = {acc[i][j][0], acc[i][j][1], acc[i][j][2], acc[i][j][3]};
@@ -451,7 +454,9 @@ __global__ __launch_bounds__(64 * WM * WN * KG, 1) void gemm_fp8_tile_kernel(Fp8
         if (m >= a.M || n >= a.N) continue;
         const uint4 v = *(const uint4*)(turn + r * PITCH + c);
         O* const to = (O*)a.y + (size_t)m * a.N + n;
-        if (n + PER <= a.N) {
+        if (aligned) {
+          __builtin_nontemporal_store(u32x4{v.x, v.y, v.z, v.w}, (u32x4*)to);
+        } else if (n + PER <= a.N) {
           __builtin_memcpy(to, &v, 16);
         } else {
           O t[PER];

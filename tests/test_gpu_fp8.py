@@ -260,3 +260,18 @@ def test_linear_same_rows_twice_give_the_same_bits():
     af.op_linear_fp8(*args, y1)
     af.op_linear_fp8(*args, y2)
     assert torch.equal(y1, y2)
+
+
+@pytest.mark.parametrize("out", ["bf16", "f32"])
+@pytest.mark.parametrize("M,N,K", [(5, 48, 128), (64, 512, 272), (282, 1024, 128), (300, 2048, 400), (1030, 777, 144), (2264, 4096, 128)])
+def test_linear_stores_at_any_alignment(out, M, N, K):
+    """The same bits wherever the results begin, and nothing before or behind them."""
+    xq, xs, wq, ws = exact_inputs(M, N, K, 7)[:4]
+    dt = DT[out]
+    want = torch.empty(M, N, dtype=dt, device="cuda")
+    af.op_linear_fp8(xq, xs, wq, ws, want)
+    for off in (1, 3, 4, 8):
+        room = torch.full((M * N + 32,), -3.0, dtype=dt, device="cuda")
+        y = room[off:off + M * N].view(M, N)
+        af.op_linear_fp8(xq, xs, wq, ws, y)
+        assert torch.equal(y, want) and bool((room[:off] == -3.0).all()) and bool((room[off + M * N:] == -3.0).all()), off
