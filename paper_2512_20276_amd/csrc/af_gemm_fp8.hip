@@ -214,7 +214,7 @@ static void stream_launch(const Fp8GemmArgs& a, hipStream_t s) {
 // stages of 40 KB as with seven of 20 KB, its products alone 27.2), so its time goes by the bytes of a
 // workgroup, (BM + BN) K.  Operands loaded straight to registers came at half that rate (55.6 us: an access
 // of 16 rows x 64 bytes takes half lines).  Large tiles are bound by the matrix cores and the scaling of
-// their results, four fma a product: 2264 x 22016 x 4096 at 2.0 PFLOP/s, the matrix cores busy half the time.
+// their results, four fma a product: 2264 x 22016 x 4096 at 2.0 PFLOP/s, the matrix cores busy 56 % of the time.
 //
 // The rows' scales come eight blocks at a time, 16 bytes a load (loaded block by block each was a request
 // of its own for 4 bytes: a third of all requests to L2), through registers into LDS, turned to [block][row].
