@@ -289,9 +289,9 @@ af_status af_op_lm_head_argmax(af_weights* w, const void* hidden, int32_t M, con
  * 8-bit form: values are e4m3 (4 exponent bits, 3 mantissa bits, largest finite value 448, no
  * infinity), times one fp32 scale for each block of 128 columns, of one row (activations) or of 128
  * rows (weights); where a size is no multiple of 128 the last block holds what is left.  A block of
- * values v is stored with the scale s = max(max |v| / 448, 2^-126) as v / s rounded to nearest even
- * (the quotient taken in fp32 first, within 2^-22 of itself); a
- * block that holds an infinity or a NaN gets a NaN scale and NaN values throughout. */
+ * values v is stored with the scale s = max(max |v| / 448, 2^-126), rounded to fp32, as v / s rounded to
+ * fp32 and then to the nearest e4m3 value, ties to even; a block that holds an infinity or a NaN gets a
+ * NaN scale and NaN values throughout. */
 
 /* Residual addition and Norm with an 8-bit result: h = x + resid, rounded to dtype and stored in
  * resid_out, then y = g * h / sqrt(mean(h^2) + eps) per row in the 8-bit form.  resid NULL (and then
