@@ -295,7 +295,8 @@ af_status af_op_lm_head_argmax(af_weights* w, const void* hidden, int32_t M, con
 
 /* Residual addition and Norm with an 8-bit result: h = x + resid, rounded to dtype and stored in
  * resid_out, then y = g * h / sqrt(mean(h^2) + eps) per row in the 8-bit form.  resid NULL (and then
- * resid_out NULL): h = x.
+ * resid_out NULL): h = x.  The root is right also where h^2 leaves fp32's range; a root below 2^-128 (eps 0
+ * and a row of subnormal numbers) gives NaN.
  *  x, resid, resid_out [M, D], g [D] of dtype (AF_BF16 or AF_F32); q [M, D] e4m3;
  *  scales fp32 [M, ceil(D / 128)].  resid_out may be resid or x itself; no other overlap.
  * Any M and D >= 1 and any alignment of the element types; M of 2^23 or more is AF_ERR_UNSUPPORTED. */

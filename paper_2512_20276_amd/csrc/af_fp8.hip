@@ -76,6 +76,31 @@ __device__ __forceinline__ uint2 pack8(const float* v, float s) {
   return make_uint2((unsigned)lo, (unsigned)hi);
 }
 
+// Eight elements in their words, for rows that are held for long: in an array of bf16, whose last chunk of a row is
+// filled one by one, each has a register of its own.
+template <typename T>
+struct Eight {
+  unsigned w[2 * sizeof(T)];
+  __device__ __forceinline__ float operator[](int e) const {
+    if constexpr (sizeof(T) == 4) return __uint_as_float(w[e]);
+    else return __uint_as_float(e & 1 ? w[e / 2] & 0xffff0000u : w[e / 2] << 16);
+  }
+};
+__device__ __forceinline__ Eight<float> eight_of(const float* v, float) {
+  Eight<float> r;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) r.w[e] = __float_as_uint(v[e]);
+  return r;
+}
+__device__ __forceinline__ Eight<bf16> eight_of(const float* v, bf16) {
+  Eight<bf16> r;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const bf16 t[2] = {from_f<bf16>(v[2 * e]), from_f<bf16>(v[2 * e + 1])};
+    __builtin_memcpy(&r.w[e], t, 4);
+  }
+  return r;
+}
 // Eight consecutive elements of a row of which n (1..8, or fewer: none) exist; the rest are zeros.
 // Whole chunks move in 16-byte accesses at any alignment that the element type allows.
 template <typename T>
@@ -88,13 +113,27 @@ __device__ __forceinline__ void load_chunk(const T* p, int n, T* v) {
   }
 }
 template <typename T>
-__device__ __forceinline__ void store_chunk(T* p, int n, const T* v) {
+__device__ __forceinline__ void load_chunk(const T* p, int n, Eight<T>& v) {
   if (n >= 8) {
-    __builtin_memcpy(p, v, 8 * sizeof(T));
+    __builtin_memcpy(v.w, p, 8 * sizeof(T));
   } else {
+    T t[8];
+    load_chunk(p, n, t);
+    __builtin_memcpy(v.w, t, 8 * sizeof(T));
+#pragma unroll
+    for (int e = 0; e < (int)(2 * sizeof(T)); ++e) asm volatile("" : "+v"(v.w[e]));  // words from here on
+  }
+}
+template <typename T>
+__device__ __forceinline__ void store_chunk(T* p, int n, const Eight<T>& v) {
+  if (n >= 8) {
+    __builtin_memcpy(p, v.w, 8 * sizeof(T));
+  } else {
+    T t[8];
+    __builtin_memcpy(t, v.w, 8 * sizeof(T));
 #pragma unroll
     for (int e = 0; e < 8; ++e)
-      if (e < n) p[e] = v[e];
+      if (e < n) p[e] = t[e];
   }
 }
 __device__ __forceinline__ void store_q(uint8_t* p, int n, uint2 q) {
@@ -112,46 +151,70 @@ __device__ __forceinline__ void store_q(uint8_t* p, int n, uint2 q) {
 // columns a thread, 16 consecutive lanes to a block of 128 columns.  The row stays in registers; a workgroup
 // that has another row to do requests it before it waits for this one's sum.  CPL = 0: longer rows, whose
 // second pass reads back what the thread itself wrote (or the input).
-// A row is added up in one order, whatever the number of rows.
+// A row is added up in one order, whatever the number of rows.  Where the sum of squares leaves fp32's range it is
+// taken again of the row times a power of two.  Three chunks a thread are kept to 128 registers, for two workgroups a
+// CU (2264 x 11008 bf16 50.7 us, with 135 registers 60.2).
 template <typename T, int WAVES, int CPL>
-__global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void add_rmsnorm_fp8_kernel(
+__global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES, CPL == 3 ? 4 : 1) void add_rmsnorm_fp8_kernel(
     const T* x, const T* resid, const T* __restrict__ g, T* resid_out, uint8_t* __restrict__ q,
     float* __restrict__ scales, int M, int D, int kb, float eps) {
   constexpr int RPW = WAVES == 1 ? 4 : 1;  // rows of a workgroup at a time
-  __shared__ float red[2][8];
+  __shared__ float red[3][8];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int c0 = WAVES == 1 ? lane : (int)threadIdx.x;
   constexpr int STEP = 64 * WAVES;
   const int n_ch = kb * 16;  // chunks of 8 columns, whole blocks of them
 
-  auto quantize = [&](size_t row, int c, const T* h, const T* gv, float inv) {
+  auto quantize = [&](size_t row, int c, const Eight<T>& h, const Eight<T>& gv, float inv) {
     const int n = D - 8 * c;
     float y[8];
     unsigned m = 0;
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      y[e] = e < n ? to_f(h[e]) * inv * to_f(gv[e]) : 0.f;
+      y[e] = h[e] * inv * gv[e];  // (past the end 0, or NaN as the whole row)
       m = max(m, abs_bits(y[e]));
     }
     const float s = scale_of(max16(m));
     if (n > 0) store_q(q + row * D + 8 * c, n, pack8(y, s));
     if ((c & 15) == 0) scales[row * kb + (c >> 4)] = s;
   };
-  // 1 / the root of the mean square, from this thread's part of the sum
-  auto norm_of = [&](float ss, int turn) {
+  // h + r, rounded as it is stored
+  auto add = [](Eight<T>& h, const Eight<T>& r) {
+    float t[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) t[e] = h[e] + r[e];
+    h = eight_of(t, T());
+  };
+  // the row's sum, from this thread's part of it
+  auto row_sum = [&](float ss, int set) {
     ss = wave_sum(ss);
     if constexpr (WAVES > 1) {
-      if (lane == 0) red[turn][wave] = ss;
+      if (lane == 0) red[set][wave] = ss;
       __syncthreads();
-      ss = red[turn][0];
+      ss = red[set][0];
 #pragma unroll
-      for (int w = 1; w < WAVES; ++w) ss += red[turn][w];
+      for (int w = 1; w < WAVES; ++w) ss += red[set][w];
     }
-    return 1.0f / sqrtf(ss / (float)D + eps);
+    return __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(ss)));  // (the same in every lane)
+  };
+  // 1 / the root of the mean square and eps, from this thread's part of the sum; scaled(f): the same part of the
+  // squares of the row times f.  A sum of 2^128 or more has an element of 2^48, so that of 2^-84 times the row has all
+  // that counts; one below 2^-96 has no element of 2^-48, and 2^100 times the row is exact.  (Set 2 is free again by the
+  // barrier of the next row's first sum.)
+  auto norm_of = [&](float ss, int turn, auto scaled) {
+    ss = row_sum(ss, turn);
+    float f = 1.0f, e = eps;
+    if (ss > 3.402823466e38f) f = 0x1p-84f;  // (or an element is infinite: the second sum is, too)
+    else if (ss < 0x1p-96f && eps < 0x1p-110f) f = 0x1p100f;
+    if (f != 1.0f) {
+      ss = row_sum(scaled(f), 2);
+      e = eps * f * f;
+    }
+    return f * (1.0f / sqrtf(ss / (float)D + e));
   };
 
   if constexpr (CPL > 0) {
-    T h[CPL][8], r[CPL][8], gv[CPL][8];
+    Eight<T> h[CPL], r[CPL], gv[CPL];
     const size_t step = (size_t)gridDim.x * RPW;
     size_t row = (size_t)blockIdx.x * RPW + (WAVES == 1 ? wave : 0);
     auto load = [&](size_t row) {
@@ -166,20 +229,28 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void add_rmsnorm_fp8
 #pragma unroll
     for (int i = 0; i < CPL; ++i) load_chunk(g + 8 * (c0 + STEP * i), D - 8 * (c0 + STEP * i), gv[i]);
     for (int turn = 0; row < (size_t)M; row += step, turn ^= 1) {  // a wave's rows are the same for all its lanes
-      T v[CPL][8];
+      Eight<T> v[CPL];
       float ss = 0.f;
 #pragma unroll
       for (int i = 0; i < CPL; ++i) {
         const int c = c0 + STEP * i, n = D - 8 * c;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          v[i][e] = resid ? from_f<T>(to_f(h[i][e]) + to_f(r[i][e])) : h[i][e];
-          ss = fmaf(to_f(v[i][e]), to_f(v[i][e]), ss);
+        v[i] = h[i];
+        if (resid) {
+          add(v[i], r[i]);
+          if (n > 0) store_chunk(resid_out + row * D + 8 * c, n, v[i]);
         }
-        if (resid && n > 0) store_chunk(resid_out + row * D + 8 * c, n, v[i]);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) ss = fmaf(v[i][e], v[i][e], ss);
       }
       load(row + step);
-      const float inv = norm_of(ss, turn);
+      const float inv = norm_of(ss, turn, [&](float f) {
+        float s = 0.f;
+#pragma unroll
+        for (int i = 0; i < CPL; ++i)
+#pragma unroll
+          for (int e = 0; e < 8; ++e) s = fmaf(v[i][e] * f, v[i][e] * f, s);
+        return s;
+      });
 #pragma unroll
       for (int i = 0; i < CPL; ++i)
         if (c0 + STEP * i < n_ch) quantize(row, c0 + STEP * i, v[i], gv[i], inv);
@@ -191,22 +262,30 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void add_rmsnorm_fp8
     float ss = 0.f;
     for (int c = c0; c < n_ch; c += STEP) {
       const int n = D - 8 * c;
-      T h[8];
+      Eight<T> h;
       load_chunk(xr + 8 * c, n, h);
       if (resid) {
-        T r[8];
+        Eight<T> r;
         load_chunk(resid + row * D + 8 * c, n, r);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) h[e] = from_f<T>(to_f(h[e]) + to_f(r[e]));
+        add(h, r);
         store_chunk(hr + 8 * c, n, h);
       }
 #pragma unroll
-      for (int e = 0; e < 8; ++e) ss = fmaf(to_f(h[e]), to_f(h[e]), ss);
+      for (int e = 0; e < 8; ++e) ss = fmaf(h[e], h[e], ss);
     }
-    const float inv = norm_of(ss, 0);
     const T* src = resid ? hr : xr;
+    const float inv = norm_of(ss, 0, [&](float f) {
+      float s = 0.f;
+      for (int c = c0; c < n_ch; c += STEP) {
+        Eight<T> h;
+        load_chunk(src + 8 * c, D - 8 * c, h);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) s = fmaf(h[e] * f, h[e] * f, s);
+      }
+      return s;
+    });
     for (int c = c0; c < n_ch; c += STEP) {
-      T h[8], gv[8];
+      Eight<T> h, gv;
       load_chunk(src + 8 * c, D - 8 * c, h);
       load_chunk(g + 8 * c, D - 8 * c, gv);
       quantize(row, c, h, gv, inv);
