@@ -312,10 +312,15 @@ af_status af_op_quantize_fp8(int32_t dtype, const void* x, void* q, float* scale
 
 /* Projection y [M, N] = x [M, K] . w [N, K]^T of 8-bit x (xq, xs with blocks of 1 x 128) and w (wq, ws
  * with blocks of 128 x 128), accumulated in fp32, y of out_dtype (AF_BF16 or AF_F32).  The sums over a
- * block are taken before its scales are applied, and a row's result does not depend on the other rows
- * except through the order of the sum over blocks, which goes by the sizes.
- * A bf16 result comes from 8-bit products, whose own error is 1.4e-5 of a result of like terms; an fp32
- * result from products that are exact.
+ * block are taken before its scales are applied.
+ * fp32 results: the products are exact, and a row's result depends on the other rows only through the
+ * order of the sum over blocks, which goes by the sizes.
+ * bf16 results: the products are exact or those of 8-bit instructions, whose own error is 1.4e-5 of a
+ * result of like terms and, where terms cancel, up to 2^-13 of the largest of eight neighbouring ones
+ * each; which of them goes by the sizes too (exact ones for most calls of up to 32 rows).  So a row
+ * alone and the same row in a batch may differ by that besides; with fp32 results they do not.
+ * The product of a block's two scales is taken in fp32: where it is below 2^-126 its bits are lost,
+ * where it is past fp32's range the result is infinite, or NaN if the block's sum is 0.
  * Any M and N >= 1.  K % 16 != 0, xq or wq not aligned to 16 bytes, K > 2^22, or 2^23 tiles of 16 x 16
  * results or more are AF_ERR_UNSUPPORTED. */
 af_status af_op_linear_fp8(const void* xq, const float* xs, const void* wq, const float* ws, void* y,

@@ -7,7 +7,13 @@
 // eight neighbouring k on a grid that ends 2^-13 below the largest of them and only the sums of eight in
 // fp32: 1.4e-5 of the result for normal values, where products in bf16 instructions (exact for e4m3
 // values) leave 1e-8.  That is 1/100 of bf16's own rounding, so a bf16 result may come from the 8-bit
-// instruction; an fp32 result never does: there the operands are widened to bf16, at half the rate.
+// instruction; an fp32 result never does: there the operands are widened to bf16, at half the rate.  The
+// kernels for few rows widen them for bf16 results as well, so the products of a row of such a result are exact
+// in a small batch and not in a large one.
+//
+// The two scales are multiplied with each other first, once for a row of 16 results (applied one by one they
+// would take four more instructions a product, beside its four fma): bits are lost where their product is below
+// 2^-126, and one past fp32's range gives infinity, or NaN for a block's sum of 0.
 #include <cmath>
 
 #include "af_device.h"
