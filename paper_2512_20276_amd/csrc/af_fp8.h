@@ -28,7 +28,7 @@ struct Fp8GemmArgs {
   void* y;           // [M, N]
   int M, N, K, kb;   // kb: blocks of 128 columns, the last one partial where K % 128 != 0
 };
-constexpr int FP8_MAX_K = 1 << 22;  // a tile of 256 rows stays below 2^30 bytes, so offsets in it fit 32 bits
+constexpr int FP8_MAX_K = 1 << 22;  // the largest tile's 288 rows take less than 2^31 bytes, so offsets in it fit 32 bits
 // Index of the kernel that a product of these sizes takes (in the lists of af_gemm_fp8.hip).
 int gemm_fp8_plan(int out_dtype, int M, int N, int K);
 hipError_t launch_gemm_fp8(int out_dtype, const Fp8GemmArgs& a, hipStream_t s);

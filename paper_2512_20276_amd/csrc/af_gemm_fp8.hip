@@ -79,11 +79,6 @@ __device__ __forceinline__ const void* uniform(const void* p) {
   return (const void*)(((uintptr_t)hi << 32) | lo);
 }
 
-// 4 bytes per lane from p + voff to LDS at dst + 4 * lane; counted by vmcnt.
-__device__ __forceinline__ void dma4(const void* p, unsigned voff, unsigned dst) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" ::"s"(dst), "v"(voff), "s"(p) : "memory");
-}
-
 // n (1..4) consecutive results of one row, rounded once.
 __device__ __forceinline__ void store4(float* p, const float* v, int n) {
   if (n >= 4) {
