@@ -52,6 +52,10 @@ class Pipeline:
     ignored.  ``prefill_ids`` is the device int32 [L_P] id pattern of every prefill (-1 for
     embedding rows).
 
+    With ``stream`` the pipeline's own device work is that stream's: its buffers are made on it, behind
+    what the current stream holds at construction, and what a step returns is ready in its order.
+    ``prefill_embeds`` is called on the current stream; its rows have to be ready in ``stream``'s order.
+
     ``sampling`` (None: greedy tokens) has tokens drawn by ``op_sample``: a dict of its settings
     (temperature, top_k, top_p, min_p), one number each for all requests.  The random numbers come
     from a generator of the pipeline's own, seeded with ``sampling_seed``; the last step's are in
@@ -73,9 +77,19 @@ class Pipeline:
         self.prefill_embeds = prefill_embeds
         self.keep_logits, self.keep_history = keep_logits, keep_history
         self.stream = stream
+        if stream is not None and prefill_ids.is_cuda:
+            stream.wait_stream(torch.cuda.current_stream(prefill_ids.device))
+            prefill_ids.record_stream(stream)
+        with torch.cuda.stream(stream):
+            self._make_buffers(prefill_ids, keep_logits, sampling, sampling_seed)
+        self.t = 0
+        self.counts: Dict[int, int] = {}
+        self.history: List[torch.Tensor] = []  # per step: device copy of its tokens
+
+    def _make_buffers(self, prefill_ids, keep_logits, sampling, sampling_seed):
         dev = prefill_ids.device
+        weights, K, P = self.w, self.K, self.P
         D = weights.shape.d_model
-        P = n_pipes
         self.M_max = P * (self.L_P + K - 1)
         self.ids = [torch.zeros(P * (self.L_P + K), dtype=torch.int32, device=dev) for _ in range(2)]
         for b in self.ids:
@@ -89,9 +103,6 @@ class Pipeline:
             self.uniforms = torch.zeros(P * K, dtype=torch.float32, device=dev)
             self.generator = torch.Generator(device=dev)
             self.generator.manual_seed(sampling_seed)
-        self.t = 0
-        self.counts: Dict[int, int] = {}
-        self.history: List[torch.Tensor] = []  # per step: device copy of its tokens
 
     def request_id(self, t: int, p: int = 0) -> int:
         return t * self.P + p
@@ -142,12 +153,13 @@ class Pipeline:
                        out_tokens if self.sampling is None else None, self.stream)
         if self.sampling is not None:
             u = self.uniforms[:n_seg]
-            with torch.cuda.stream(self.stream):
+            with torch.cuda.stream(self.stream):  # (None: the current one)
                 u.uniform_(generator=self.generator)
             op_sample(logits, u, out_tokens, **{what: v[:n_seg] for what, v in self.sampling.items()}, stream=self.stream)
         done = self.finish(segs)
         if self.keep_history:
-            self.history.append(out_tokens.clone())
+            with torch.cuda.stream(self.stream):
+                self.history.append(out_tokens.clone())
         self.t += 1
         return StepResult(t=t, M=M, segments=[s.astuple() for s in segs], tokens=out_tokens,
                           hidden=self.hidden[:M], logits=logits if self.keep_logits else None,
@@ -155,6 +167,8 @@ class Pipeline:
 
     def request_tokens(self, r: int, p: int = 0) -> List[int]:
         """Tokens generated so far for request r of pipeline p (host copy; synchronizes)."""
+        if self.stream is not None:
+            self.stream.synchronize()
         out = []
         for s in range(self.K):
             t = r + s
