@@ -111,7 +111,8 @@ class NaivePipeline:
         n_seg = len(segs)
         op_lm_head_argmax(self.w, hidden, arr, self.logits[:n_seg] if self.logits is not None else None,
                           self.tokens[:n_seg], self.stream)
-        toks = self.tokens[:n_seg].cpu().tolist()  # synchronizes: the host builds the next batch
+        with torch.cuda.stream(self.stream):  # (None: the current one)
+            toks = self.tokens[:n_seg].cpu().tolist()  # synchronizes: the host builds the next batch
         done = None
         for seg, tok in zip(segs, toks):
             self.counts[seg.request_id] = seg.pos0 + seg.q_len

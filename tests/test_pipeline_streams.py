@@ -9,6 +9,7 @@ import torch
 import workload as wl
 
 af = pytest.importorskip("paper_2512_20276_amd")
+from paper_2512_20276_amd import naive_pipe as npipe  # noqa: E402
 from paper_2512_20276_amd import pipeline as pl  # noqa: E402
 
 
@@ -68,6 +69,23 @@ def test_device_work_goes_to_the_stream_of_the_pipeline(monkeypatch, sampling, o
     assert log == [("embeds", "caller's")] + ([("uniform_", at)] if sampling else []) + [("clone", at)]
     pipe.request_tokens(0)
     assert (("sync", "mine") in streams.log) == own
+
+
+@pytest.mark.parametrize("own", [True, False])
+def test_naive_pipeline_reads_its_tokens_on_its_stream(monkeypatch, own):
+    w = types.SimpleNamespace(shape=wl.TINY, dtype=torch.float32)
+    staging = af.Ring(0, 2, 16)
+    staging.copy_kv_to = lambda *a: None
+    monkeypatch.setattr(npipe, "Ring", lambda *a: staging)
+    for name in ("op_embed", "packed_layer_forward", "op_lm_head_argmax"):
+        monkeypatch.setattr(npipe, name, lambda *a, **kw: None)
+    stream = types.SimpleNamespace(synchronize=lambda: None) if own else None
+    pipe = npipe.NaivePipeline(w, 2, torch.full((4,), -1, dtype=torch.int32), lambda t: torch.zeros(5, 4), False, stream=stream)
+    pipe.tokens.zero_()
+    streams = Streams(monkeypatch)
+    monkeypatch.setattr(torch.Tensor, "cpu", streams.noted("cpu", torch.Tensor.cpu))
+    pipe.step()
+    assert [e for e in streams.log if e[0] == "cpu"] == [("cpu", stream if own else "caller's")]
 
 
 @pytest.mark.gpu
