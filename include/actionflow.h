@@ -338,8 +338,9 @@ af_status af_op_linear_fp8(const void* xq, const float* xs, const void* wq, cons
  *  uniforms [n_rows] in [0, 1); below it counts as 0, 1 and above draw the last kept token.
  *  tokens   [n_rows].
  * A logit of -inf or NaN is never drawn; a row that has no other gives token 0, as the greedy head
- * does.  Logits of +inf share the row.  Weights below 2^-41 count as 0.  The sums are exact, so a
- * row's token depends on nothing but that row.  vocab > 2^22 or n_rows of 2^22 or more is
+ * does.  Logits of +inf share the row.  Weights are taken to the nearest multiple of 2^-40 of the
+ * first token's, so ones below 2^-41 count as 0; their sums are exact, so a row's token depends on
+ * nothing but that row.  vocab > 2^22 or n_rows of 2^22 or more is
  * AF_ERR_UNSUPPORTED. */
 af_status af_op_sample(int32_t dtype, const void* logits, int32_t n_rows, int32_t vocab, const float* temperature,
                        const int32_t* top_k, const float* top_p, const float* min_p, const float* uniforms,
