@@ -210,12 +210,14 @@ static void stream_launch(const Fp8GemmArgs& a, hipStream_t s) {
 // 16-byte chunk c sits at place c ^ (row % 8), so that neither the 16 rows that an operand read touches
 // nor the 8 of a load meet on a bank.
 //
-// What bounds it: a tile of few rows takes its operands into LDS at about 30 bytes a clock and CU, however
-// many stages are under way (282 x 4096 x 11008 on 96 x 64 tiles: 34.8 us; its loads alone 28.0, the same with three
-// stages of 40 KB as with seven of 20 KB, its products alone 27.2), so its time goes by the bytes of a
-// workgroup, (BM + BN) K.  Operands loaded straight to registers came at half that rate (55.6 us: an access
-// of 16 rows x 64 bytes takes half lines).  Large tiles are bound by the matrix cores and the scaling of
-// their results, four fma a product: 2264 x 22016 x 4096 at 2.0 PFLOP/s, the matrix cores busy 56 % of the time.
+// What bounds it: a tile of few rows takes its operands into LDS at about 30 bytes a clock and CU (282 x 4096 x
+// 11008 on 96 x 64 tiles: 32.2 us; in an earlier loop of 34.8 its loads alone took 28.0 and its products alone 27.2), so its
+// time goes by the bytes of a workgroup, (BM + BN) K.  More stages under way were no faster (three of 40 KB, seven of
+// 20 KB), but this loop cannot tell: the rows' scales pass through registers, whose loads the compiler waits for together
+// with every load to LDS behind them, in the first and the last stage of a set of scales.  Operands loaded straight to
+// registers came at half the rate (55.6 us: an access of 16 rows x 64 bytes takes half lines).  Large tiles are bound by the
+// matrix cores and the scaling of their results, four fma a product, and by the last pass of the GPU over them, which is
+// seldom full: 2264 x 22016 x 4096 at 2.0 PFLOP/s, the matrix cores busy 56 % of the time, 688 tiles on 256 CUs.
 //
 // The rows' scales come eight blocks at a time, 16 bytes a load (loaded block by block each was a request
 // of its own for 4 bytes: a third of all requests to L2), through registers into LDS, turned to [block][row].
@@ -433,15 +435,15 @@ __global__ __launch_bounds__(64 * WM * WN * KG, 1) void gemm_fp8_tile_kernel(Fp8
     });
   } else {
     // A lane's four results of a row are a quarter or half of a line.  So the results of 16 rows are turned in LDS of
-    // the wave's own, and a store takes rows of 16 CN columns: whole lines where CN = 4 (2264 x 22016 x 4096:
-    // 205 us, four results a store 219; 208 x 22016 x 128 to fp32: 8.4 and 14.2).
+    // the wave's own, and a store takes rows of 16 CN columns: whole lines where CN = 4 (through L2, 2264 x
+    // 22016 x 4096 took 205 us so and 219 with four results a store, 208 x 22016 x 128 to fp32 8.4 and 14.2).
     constexpr int PER = 16 / sizeof(O), ROW = 16 * CN, PITCH = ROW + PER;  // of a 16-byte piece, a row, and padded
     constexpr int PIECES = ROW / PER;
     static_assert(S::RED + WM * WN * 16 * PITCH * (int)sizeof(O) <= (int)sizeof(smem), "LDS");
     O* const turn = (O*)(smem + S::RED) + (wn * WM + wm) * (16 * PITCH);  // behind the sums that others still read
     const int n0w = n0 + wn * ROW;
     // Past L2 where the pieces are aligned: no line of the results is read before the next launch, which does not
-    // find it in L2 (282 x 22016 x 4096 50.9 us, through L2 51.6; 208 x 22016 x 128 to fp32 7.0 and 8.4).
+    // find it in L2 (208 x 22016 x 128 to fp32 7.1 us, through L2 8.4; 282 x 22016 x 4096 1 % faster).
     const bool aligned = a.N % PER == 0 && (uintptr_t)a.y % 16 == 0;
     static_for<0, RM>([&](auto i) {
       static_for<0, CN>([&](auto j) {
@@ -484,16 +486,18 @@ static void tile_launch(const Fp8GemmArgs& a, hipStream_t s) {
 // whole), stages of its K loop in each of them, and the stages and results of the whole work where
 // the GPU is busy (in units of a full pass: L2 and HBM then set the pace of a stage).  Coefficients are a
 // least-squares fit to 21 row counts (1..2264) of 10 weight shapes (512 x 4096 .. 32000 x 4096, K 512 ..
-// 11008), for fp32 results also to 10 of 5 shapes with K 64 .. 256.  The variant of the least estimate takes
-// 1.5 % longer than the fastest one timed on the mean (fp32 0.7 %), 24 % at the worst; with K of 256 and
-// less, where a call takes 3 to 20 us, 7 % (fp32 2 %).  Measured, us, against the next variants:
+// 11008), for fp32 results also to 10 of 5 shapes with K 64 .. 256.  The bf16 ones were fitted before results were
+// turned in LDS and stored past L2; fitted anew to all of these shapes they choose as well (2.4 % on the mean).  Against
+// the fastest kernel for these 263 shapes the one of the least estimate takes 1.4 % longer on the mean for K of 512 and more
+// (24 % at the worst: 16 x 12288 x 4096; fp32 results 0.6 and 16 %), and 7 % for K of 256 and less (66 %: 7 x 22016 x 144,
+// 5.3 us for 3.2; fp32 2.5 and 28 %).  Measured, us, bf16 results, against the next variants:
 //   rows x columns x K       taken                      others
-//   7 x 32000 x 4096         16 x 32 streamed 25.7      64 x 64 27.0, 16 x 16 streamed 30.5
-//   64 x 4096 x 4096         32 x 32, four groups 10.4  32 x 64 11.7, 64 x 64 13.4
-//   282 x 4096 x 11008       96 x 64, two groups 32.9   64 x 64 40.1, 128 x 128 52.6
-//   282 x 22016 x 4096       160 x 256 53.9             256 x 256 54.5, 128 x 256 60.3
-//   1024 x 4096 x 4096       128 x 128, two groups 25.4 160 x 128 26.8, 128 x 256 31.3
-//   2264 x 22016 x 4096      288 x 256 219              256 x 256 226, 128 x 256 237
+//   7 x 32000 x 4096         16 x 32 streamed 26.4      64 x 64 30.0, 16 x 16 streamed 30.1
+//   64 x 4096 x 4096         32 x 32, four groups 10.6  32 x 64 11.6, 64 x 64 13.3
+//   282 x 4096 x 11008       96 x 64, two groups 32.2   64 x 64 39.0, 128 x 128 52.1
+//   282 x 22016 x 4096       160 x 256 45.8             256 x 256 49.4, 160 x 128 55.7
+//   1024 x 4096 x 4096       128 x 128, two groups 24.6 160 x 128 25.6, 128 x 256 29.3
+//   2264 x 22016 x 4096      288 x 256 197              256 x 256 222, 128 x 256 226
 // The streamed ones (K split over the waves, operands straight to registers) are for up to 32 rows: past
 // that they read the activations again for every 16 or 32 columns.
 struct Fp8Variant {
