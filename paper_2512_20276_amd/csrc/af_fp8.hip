@@ -7,7 +7,7 @@
 // q = NaN throughout, so that nothing computed from it looks finite.  The quotient is the one that rounding
 // v / s to fp32 gives, from a reciprocal that the block's elements share: bf16 elements over a bf16 maximum
 // often lie midway between two e4m3 values, where an ulp decides (v times the reciprocal instruction's 1 / s
-// alone took the other value for up to 4 in 10^3 of bf16 elements).  (With the division itself, ten
+// alone took the other value for 1.3 to 1.7 in 10^3 of bf16 elements).  (With the division itself, ten
 // instructions an element, 22016 x 4096 weights took 59.5 us, bound by them; so 54.5.)
 //
 // Every kernel here reads its input once, in 16-byte accesses, and is bound by memory: what it holds of a
