@@ -28,6 +28,7 @@
 #ifndef ACTIONFLOW_H
 #define ACTIONFLOW_H
 
+#include <stddef.h>
 #include <stdint.h>
 
 #ifdef __cplusplus
@@ -345,6 +346,70 @@ af_status af_op_linear_fp8(const void* xq, const float* xs, const void* wq, cons
 af_status af_op_sample(int32_t dtype, const void* logits, int32_t n_rows, int32_t vocab, const float* temperature,
                        const int32_t* top_k, const float* top_p, const float* min_p, const float* uniforms,
                        int32_t* tokens, void* hip_stream);
+
+/* ------------------------------------------------------------------ paged key-value cache
+ * For programs whose requests keep their keys and values in pages of one pool instead of ring slots: the
+ * rotation and write of a step's rows, and the attention of these rows over the pages.  Not steps of the
+ * paper's method.  Neither allocates, waits or keeps anything between calls, so they run on any stream and
+ * under graph capture; what they find out about the requests they read on the device when they run, so a
+ * captured call replays with the lengths, tables and positions that are there then.  What is written overlaps
+ * nothing else unless said so. */
+
+/* The pool, and the requests of one step.  Key j of request b is at offset j % page_size of page
+ * page_table[b][j / page_size].  Request b has the packed rows q_starts[b] .. q_starts[b + 1] - 1 (ascending;
+ * without q_starts there is one row a request, row b) and kv_lens[b] keys with them: row i of its n has cache
+ * position p = kv_lens[b] - n + i.
+ *  - k and v are aligned to 16 bytes; the layers of a model are pools of their own, or parts of one allocation.
+ *  - A request may have no rows, and its length may be 0; packed rows of no request (padding before the first
+ *    start or from the last one on) are neither read nor written.
+ *  - Keys past kv_lens are not read into any result, whatever the pages hold there.  Keys on a page number
+ *    outside [0, n_pages), or past the table, do not exist: they are not written, and nothing sees them.
+ *    Requests may share pages that they only read.
+ *  - AF_ERR_UNSUPPORTED: head_dim other than 64 and 128; a page_size that is no power of two or below 8; more
+ *    than 2^30 keys in max_pages; M * n_heads of 2^30 or more; n_seq * max_pages * page_size / 32 past 2^31. */
+typedef struct af_paged_kv {
+  void* k;                   /* device [n_pages][n_kv_heads][page_size][head_dim] of dtype */
+  void* v;                   /* likewise */
+  const int32_t* page_table; /* device [n_seq][max_pages] */
+  const int32_t* kv_lens;    /* device [n_seq] */
+  const int32_t* q_starts;   /* device [n_seq + 1], or NULL */
+  int32_t n_pages, page_size, n_kv_heads, head_dim, n_seq, max_pages;
+  int32_t dtype;    /* af_dtype */
+  int32_t reserved; /* must be 0 */
+} af_paged_kv;
+
+/* Rotates the queries and keys of M packed rows and writes keys and values to their pages.
+ *  q, q_out [M][n_heads][head_dim]; k, v [M][n_kv_heads][head_dim] of the cache's dtype, the heads of a row
+ *  side by side and the rows *_stride elements apart, so that the three may be parts of one projection's rows;
+ *  q_out may be q (with its stride).  Rows are aligned to 16 bytes, else AF_ERR_UNSUPPORTED.
+ *  positions device [M][n_axes], any int32, or NULL (n_axes 1): the cache positions.
+ *  sections  host [n_axes]: how many pairs of a head turn with each axis, in order, head_dim / 2 in all (time,
+ *            height and width of image patches, say); NULL for one axis.
+ * Pair (j, j + head_dim / 2) turns by position * theta^(-2j / head_dim), as in the packed forward; the angle is
+ * taken in 64 bits and each result rounded once.  Rows are independent; of two rows written to the same cell
+ * (a page that two requests write) either may remain. */
+af_status af_op_rope_append_paged(const af_paged_kv* kv, const void* q, int64_t q_stride, const void* k,
+                                  int64_t k_stride, const void* v, int64_t v_stride, const int32_t* positions,
+                                  const int32_t* sections, int32_t n_axes, float theta, void* q_out,
+                                  int64_t q_out_stride, int32_t M, int32_t n_heads, void* hip_stream);
+
+/* Bytes of device workspace that af_op_attention_paged needs for these sizes (the cache's and its requests',
+ * whether q_starts is there, M and n_heads; no pointer is followed).  It may be 0. */
+af_status af_attention_paged_workspace(const af_paged_kv* kv, int32_t M, int32_t n_heads, size_t* bytes);
+
+/* o = softmax(scale * q . k^T) v for M packed rows (rotated queries q [M][n_heads][head_dim], o likewise, rows
+ * as above) over the pages.  Heads share key heads in groups of n_heads / n_kv_heads, in order.
+ * Row p of a request sees its keys j <= p; with a window > 0 only those with j > p - window, and the first n_sink
+ * (without a window n_sink means nothing).  A row that sees nothing gives zeros.
+ *  lse  device fp32 [M][n_heads] or NULL: the natural logarithm of a row's sum of exponentials of
+ *       scale * q . k (-inf where it sees nothing), with which results over parts of a history can be joined.
+ *  workspace  of af_attention_paged_workspace bytes, aligned to 16; its contents before and after mean nothing.
+ *       Calls that may run at the same time need one each (so do graphs that replay at the same time).
+ * Scores, sums and outputs are held in fp32.  A row's result may depend on the other rows through the order of
+ * its sums, which goes by the lengths of all requests; it is the same for every run with the same sizes. */
+af_status af_op_attention_paged(const af_paged_kv* kv, const void* q, int64_t q_stride, void* o, int64_t o_stride,
+                                float* lse, int32_t M, int32_t n_heads, float scale, int32_t window, int32_t n_sink,
+                                void* workspace, size_t workspace_bytes, void* hip_stream);
 
 /* ------------------------------------------------------------------ timing
  * Kernel classes for per-kernel timing with HIP events recorded on the launch stream. */

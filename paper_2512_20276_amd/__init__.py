@@ -56,6 +56,13 @@ class Segment(C.Structure):
                 f"request_id={self.request_id}, flags={self.flags})")
 
 
+class PagedKVDesc(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("page_table", C.c_void_p), ("kv_lens", C.c_void_p),
+                ("q_starts", C.c_void_p), ("n_pages", C.c_int32), ("page_size", C.c_int32), ("n_kv_heads", C.c_int32),
+                ("head_dim", C.c_int32), ("n_seq", C.c_int32), ("max_pages", C.c_int32), ("dtype", C.c_int32),
+                ("reserved", C.c_int32)]
+
+
 def _load():
     if not os.path.exists(LIB_PATH):
         raise ImportError(f"{LIB_PATH} is not built; run `python paper_2512_20276_amd/build.py` "
@@ -97,6 +104,9 @@ def _load():
         "af_op_quantize_fp8": (I32, [I32, P, P, P, I32, I32, I32, P]),
         "af_op_linear_fp8": (I32, [P, P, P, P, P, I32, I32, I32, I32, P]),
         "af_op_sample": (I32, [I32, P, I32, I32, P, P, P, P, P, P, P]),
+        "af_op_rope_append_paged": (I32, [P, P, I64, P, I64, P, I64, P, P, I32, F32, P, I64, I32, I32, P]),
+        "af_attention_paged_workspace": (I32, [P, I32, I32, C.POINTER(C.c_size_t)]),
+        "af_op_attention_paged": (I32, [P, P, I64, P, I64, P, I32, I32, F32, I32, I32, P, C.c_size_t, P]),
         "af_weights_set_options": (I32, [P, U32]),
         "af_timing_enable": (I32, [P, U32]),
         "af_timing_read": (I32, [P, C.POINTER(C.c_double), C.POINTER(I64)]),
@@ -446,3 +456,84 @@ def op_sample(logits: torch.Tensor, uniforms: torch.Tensor, tokens: torch.Tensor
         at.append(None if t is None else t.data_ptr())
     _call_on(dev, stream, lib.af_op_sample, dtype_code(logits.dtype), logits.data_ptr(), n, V, *at,
              uniforms.data_ptr(), tokens.data_ptr())
+
+
+# ----------------------------------------------------------------------------- paged key-value cache
+class PagedKV:
+    """A pool of pages and the requests of one step, as the operators below take them.
+
+    ``k``, ``v`` [n_pages, n_kv_heads, page_size, head_dim] (bf16 or fp32); ``page_table`` int32 [n_seq, max_pages];
+    ``kv_lens`` int32 [n_seq], lengths with this step's rows; ``q_starts`` int32 [n_seq + 1], first packed row of each
+    request and the end of the last one's, or None: one row a request.  The tensors are held, not copied: their
+    values may change between calls (and between replays of a captured one), their storage may not."""
+
+    def __init__(self, k: torch.Tensor, v: torch.Tensor, page_table: torch.Tensor, kv_lens: torch.Tensor,
+                 q_starts: Optional[torch.Tensor] = None):
+        if k.dim() != 4 or page_table.dim() != 2:
+            raise ValueError("k must be [n_pages, n_kv_heads, page_size, head_dim], page_table [n_seq, max_pages]")
+        self.device, self.dtype, i32 = k.get_device(), k.dtype, torch.int32
+        _want("k", k, k.shape, k.dtype, self.device)
+        _want("v", v, k.shape, k.dtype, self.device)
+        n_seq, max_pages = page_table.shape
+        _want("page_table", page_table, (n_seq, max_pages), i32, self.device)
+        _want("kv_lens", kv_lens, (n_seq,), i32, self.device)
+        if q_starts is not None:
+            _want("q_starts", q_starts, (n_seq + 1,), i32, self.device)
+        self.k, self.v, self.page_table, self.kv_lens, self.q_starts = k, v, page_table, kv_lens, q_starts
+        n_pages, self.n_kv_heads, page_size, self.head_dim = k.shape
+        self.desc = PagedKVDesc(k.data_ptr(), v.data_ptr(), page_table.data_ptr(), kv_lens.data_ptr(),
+                                None if q_starts is None else q_starts.data_ptr(), n_pages, page_size, self.n_kv_heads,
+                                self.head_dim, n_seq, max_pages, dtype_code(k.dtype), 0)
+        self.ref = C.addressof(self.desc)
+
+    def _rows(self, what: str, t: torch.Tensor, M: int, n_heads: int) -> int:
+        """Elements between the rows of ``t`` [M, n_heads, head_dim], whose heads lie side by side."""
+        hd = self.head_dim
+        if (t.dtype is not self.dtype or t.get_device() != self.device or t.shape != (M, n_heads, hd) or t.stride(2) != 1
+                or (n_heads > 1 and t.stride(1) != hd)):
+            raise ValueError(f"{what} must be a {self.dtype} tensor of shape {(M, n_heads, hd)} with the heads of a row side "
+                             f"by side, on the cache's device, got {t.dtype} {tuple(t.shape)} {t.stride()} on {t.device}")
+        return t.stride(0) if M > 1 else n_heads * hd
+
+
+def op_rope_append_paged(kv: PagedKV, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, q_out: torch.Tensor,
+                         theta: float, positions: Optional[torch.Tensor] = None,
+                         sections: Optional[Sequence[int]] = None, stream=None):
+    """Rotates ``q`` [M, n_heads, head_dim] into ``q_out`` (which may be q) and writes rotated ``k`` and ``v``
+    [M, n_kv_heads, head_dim] to their pages; rows of any stride, as parts of one projection have it.  ``positions``
+    int32 [M] or [M, n_axes] (None: cache positions); ``sections``: pairs of a head that turn with each axis."""
+    M, n_heads = q.shape[:2]
+    n_axes = 1
+    if positions is not None:
+        n_axes = 1 if positions.dim() == 1 else positions.shape[1]
+        _want("positions", positions, (M,) if positions.dim() == 1 else (M, n_axes), torch.int32, kv.device)
+    if sections is not None and len(sections) != n_axes:
+        raise ValueError(f"sections are of {len(sections)} axes, positions of {n_axes}")
+    _call_on(kv.device, stream, lib.af_op_rope_append_paged, kv.ref, q.data_ptr(), kv._rows("q", q, M, n_heads),
+             k.data_ptr(), kv._rows("k", k, M, kv.n_kv_heads), v.data_ptr(), kv._rows("v", v, M, kv.n_kv_heads),
+             None if positions is None else positions.data_ptr(),
+             None if sections is None else (C.c_int32 * n_axes)(*sections), n_axes, theta, q_out.data_ptr(),
+             kv._rows("q_out", q_out, M, n_heads), M, n_heads)
+
+
+def attention_paged_workspace(kv: PagedKV, M: int, n_heads: int) -> int:
+    """Bytes of workspace that ``op_attention_paged`` needs for M rows of n_heads heads."""
+    n = C.c_size_t()
+    _check(lib.af_attention_paged_workspace(kv.ref, M, n_heads, C.byref(n)))
+    return n.value
+
+
+def op_attention_paged(kv: PagedKV, q: torch.Tensor, o: torch.Tensor, scale: float, workspace: Optional[torch.Tensor],
+                       window: int = 0, n_sink: int = 0, lse: Optional[torch.Tensor] = None, stream=None):
+    """``o`` [M, n_heads, head_dim] <- attention of rotated queries ``q`` over the pages, causal within each request; with
+    a ``window`` a row sees the last ``window`` keys and the first ``n_sink``.  ``workspace``: a uint8 tensor of
+    ``attention_paged_workspace`` bytes (None where that is 0); ``lse`` fp32 [M, n_heads]: log of the sums."""
+    M, n_heads = q.shape[:2]
+    if lse is not None:
+        _want("lse", lse, (M, n_heads), torch.float32, kv.device)
+    if workspace is not None:
+        _want("workspace", workspace, workspace.shape, torch.uint8, kv.device)
+    _call_on(kv.device, stream, lib.af_op_attention_paged, kv.ref, q.data_ptr(), kv._rows("q", q, M, n_heads), o.data_ptr(),
+             kv._rows("o", o, M, n_heads), None if lse is None else lse.data_ptr(), M, n_heads, scale, window, n_sink,
+             None if workspace is None or workspace.numel() == 0 else workspace.data_ptr(),
+             0 if workspace is None else workspace.numel())

@@ -1,0 +1,294 @@
+// Device code that the kernels over a paged cache share: where a request's rows and keys are, and the
+// attention of 16 query columns over a tile of 32 keys that one wave holds in registers.
+#pragma once
+
+#include "af_device.h"
+#include "af_paged.h"
+
+namespace af {
+
+constexpr int KEY_TILE = 32;
+constexpr int NO_WINDOW = 0x7fffffff;
+
+struct Request {
+  int first, n, len;  // rows [first, first + n), cache length with them
+};
+// Rows are cut to the packed ones and lengths to 0 and more, so that no table makes a kernel leave its buffers.
+__device__ __forceinline__ Request request_at(const PagedCache& c, int b) {
+  Request r{b, 1, max(c.lens[b], 0)};
+  if (c.starts) {
+    r.first = min(max(c.starts[b], 0), c.M);
+    r.n = min(max(c.starts[b + 1], r.first), c.M) - r.first;
+  }
+  return r;
+}
+
+// The request that a row belongs to, -1: none.  Called by whole waves with one row.
+__device__ __forceinline__ int request_of_row(const PagedCache& c, int row) {
+  if (!c.starts) return row < c.n_seq ? row : -1;
+  const int lane = threadIdx.x & 63;
+  if (row < c.starts[0]) return -1;
+  for (int b0 = 0; b0 < c.n_seq; b0 += 64) {
+    const int b = b0 + lane;
+    const unsigned long long past = __ballot(b < c.n_seq && c.starts[min(b, c.n_seq - 1) + 1] > row);
+    if (past) return b0 + __builtin_ctzll(past);
+  }
+  return -1;
+}
+
+// Keys that positions lowest .. highest can see: [0, sink_end) and [lo, end), as tiles of KEY_TILE keys.
+// Tiles 0 .. n_sink - 1 are those of the first keys, the others lie from key tile `first` on; where the two
+// would meet there are no separate first ones.
+struct KeyTiles {
+  int n_sink, first, n;
+  __device__ __forceinline__ int key(int i) const { return (i < n_sink ? i : first + i - n_sink) * KEY_TILE; }
+};
+__device__ __forceinline__ KeyTiles key_tiles(const PagedAttnArgs& a, int lowest, int highest) {
+  const int end = min(highest, a.c.cap - 1) + 1;  // a position of -1 or less sees nothing
+  const int lo = min(max(max(lowest, -1) - a.window + 1, 0), max(end, 0));
+  KeyTiles t;
+  t.first = lo / KEY_TILE;
+  t.n_sink = (min(a.sinks, lo) + KEY_TILE - 1) / KEY_TILE;
+  if (t.n_sink >= t.first) t.n_sink = t.first = 0;
+  t.n = end <= 0 ? 0 : t.n_sink + (end + KEY_TILE - 1) / KEY_TILE - t.first;
+  return t;
+}
+// (The clamp keeps p - window within 32 bits where there is none.)
+__device__ __forceinline__ bool sees(const PagedAttnArgs& a, int p, int j) {
+  return j <= p && j < a.c.cap && (j > max(p, -1) - a.window || j < a.sinks);
+}
+
+// The page of key j0 + lane % 32, -1 where there is none.
+__device__ __forceinline__ int page_of(const PagedCache& c, int b, int j0) {
+  const int j = j0 + (threadIdx.x & 31);
+  const int at = j >> c.page_shift;
+  const int page = c.table[(size_t)b * c.max_pages + min(at, c.max_pages - 1)];
+  return at < c.max_pages && page >= 0 && page < c.n_pages ? page : -1;
+}
+
+// Softmax state and output of 16 columns, one for each lane % 16.  Scores are taken transposed, S^T = K . Q^T, and so is
+// the output, O^T = V^T . P^T: of both a lane then holds its own column alone (four lanes share one), the
+// probabilities are the product's operand as they are, and maximum, sum and scaling need no exchange but two
+// steps over the four lanes.  A lane's output of group j is element i of head dimensions (4 g + i) VJ + j.
+template <typename T, int HD>
+struct Columns {
+  static constexpr int KST = HD / 32, VJ = HD / 16;
+  typedef typename Mma<T>::frag frag;
+  frag q[KST];
+  f32x4 o[VJ];
+  float m, l;
+
+  __device__ __forceinline__ void clear() {
+#pragma unroll
+    for (int j = 0; j < VJ; ++j) o[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    m = -INFINITY;
+    l = 0.f;
+  }
+  // row: the lane's column, null: none
+  __device__ __forceinline__ void load_q(const T* row) {
+    const int lg = (threadIdx.x & 63) >> 4;
+#pragma unroll
+    for (int s = 0; s < KST; ++s) {
+      T t[8] = {};
+      if (row) load8(row + s * 32 + lg * 8, t);
+      __builtin_memcpy(&q[s], t, sizeof(q[s]));
+    }
+  }
+  __device__ __forceinline__ float sum() const {  // of the four lanes' sums
+    const float s = l + __shfl_xor(l, 16);
+    return s + __shfl_xor(s, 32);
+  }
+};
+
+__device__ __forceinline__ bool not_finite(bf16 x) { return (__builtin_bit_cast(unsigned short, x) & 0x7f80) == 0x7f80; }
+__device__ __forceinline__ bool not_finite(float x) { return (__float_as_uint(x) & 0x7f800000u) == 0x7f800000u; }
+
+// One tile of keys j0 .. j0 + 31 of key head hk, whose pages the lanes hold (page_of).  p: the position of the lane's
+// column; lowest, highest: of all columns.  MANY: columns of several positions.
+// A lane loads 16 bytes of a key in each of KST steps, and its VJ values of eight keys: the keys 4 g .. 4 g + 3 of
+// either half of the tile, whose probabilities it holds.  Values that no column sees are replaced by zeros, since a
+// probability of 0 does not hide an infinity or a NaN; where only some columns see a value that is not finite the products
+// are taken one by one.
+// With bf16 values a probability is split into a bf16 head and a bf16 remainder, two products, so that it keeps
+// 16 bits: the cache's bytes bound these kernels, not the matrix instructions.
+template <typename T, int HD, bool MANY>
+__device__ __forceinline__ void attend_tile(const PagedAttnArgs& a, int hk, int j0, int page, int p, int lowest, int highest,
+                                            Columns<T, HD>& c) {
+  typedef Columns<T, HD> C;
+  typedef typename C::frag frag;
+  constexpr int KST = C::KST, VJ = C::VJ;
+  const int lane = threadIdx.x & 63, lr = lane & 15, lg = lane >> 4;
+  const int in_page = (1 << a.c.page_shift) - 1;
+  const size_t page_rows = (size_t)a.c.n_kv_heads << a.c.page_shift, head_row = (size_t)hk << a.c.page_shift;
+  const T* K = (const T*)a.c.k;
+  const T* V = (const T*)a.c.v;
+  frag kf[2][KST];
+  T v[8][VJ];
+  int of_page[2];
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const int kp = max(__shfl(page, h * 16 + lr), 0);
+    const T* krow = K + (kp * page_rows + head_row + ((j0 + h * 16 + lr) & in_page)) * HD + lg * 8;
+#pragma unroll
+    for (int s = 0; s < KST; ++s) kf[h][s] = *(const frag*)(krow + s * 32);
+  }
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    of_page[h] = __shfl(page, h * 16 + lg * 4);
+    const T* vrow = V + (max(of_page[h], 0) * page_rows + head_row + ((j0 + h * 16 + lg * 4) & in_page)) * HD + lr * VJ;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) __builtin_memcpy(v[h * 4 + i], __builtin_assume_aligned(vrow + i * HD, VJ * sizeof(T)), VJ * sizeof(T));
+  }
+
+  float s[8];
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    f32x4 acc = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int t = 0; t < KST; ++t) acc = Mma<T>::mma(kf[h][t], c.q[t], acc);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) s[h * 4 + i] = acc[i] * a.scale_log2;
+  }
+  const bool whole = sees(a, lowest, j0 + KEY_TILE - 1) && (j0 > max(highest, -1) - a.window || j0 + KEY_TILE <= a.sinks) &&
+                     __all(page >= 0);
+  bool one_by_one = false;
+  if (!whole) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const int j = j0 + (e >> 2) * 16 + lg * 4 + (e & 3);
+      const bool there = of_page[e >> 2] >= 0;
+      if (!there || !sees(a, p, j)) s[e] = -INFINITY;
+      const bool some = MANY ? there && j <= highest && j < a.c.cap && (j > max(lowest, -1) - a.window || j < a.sinks)
+                             : there && sees(a, p, j);
+#pragma unroll
+      for (int d = 0; d < VJ; ++d) {
+        if (!some) v[e][d] = from_f<T>(0.f);
+        if (MANY) one_by_one |= not_finite(v[e][d]);
+      }
+    }
+    if (MANY) one_by_one = __any(one_by_one);
+  }
+
+  float top = s[0];
+#pragma unroll
+  for (int e = 1; e < 8; ++e) top = fmaxf(top, s[e]);
+  top = fmaxf(top, __shfl_xor(top, 16));
+  top = fmaxf(top, __shfl_xor(top, 32));
+  const float m = fmaxf(c.m, top);
+  const float ref = m == -INFINITY ? 0.f : m;  // no key seen yet: probabilities and factor come out 0
+  if (__any(m > c.m)) {
+    const float f = __builtin_amdgcn_exp2f(c.m - ref);
+    c.l *= f;
+#pragma unroll
+    for (int j = 0; j < VJ; ++j) c.o[j] *= f;
+    c.m = m;
+  }
+  frag pf, pl;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    s[e] = __builtin_amdgcn_exp2f(s[e] - ref);
+    c.l += s[e];
+    pf[e] = from_f<T>(s[e]);
+    pl[e] = from_f<T>(s[e] - to_f(pf[e]));
+  }
+  if (!MANY || !one_by_one) {
+#pragma unroll
+    for (int j = 0; j < VJ; ++j) {
+      frag vf;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) vf[e] = v[e][j];
+      c.o[j] = Mma<T>::mma(vf, pf, c.o[j]);
+      if constexpr (sizeof(T) == 2) c.o[j] = Mma<T>::mma(vf, pl, c.o[j]);
+    }
+    return;
+  }
+#pragma unroll
+  for (int e = 0; e < 8; ++e)
+#pragma unroll 1
+    for (int g = 0; g < 4; ++g) {
+      const int at = (e >> 2) * 16 + g * 4 + (e & 3), j = j0 + at;
+      const float w = __shfl(s[e], g * 16 + lr);
+      const int kp = __shfl(page, at);
+      if (kp < 0 || !sees(a, p, j)) continue;
+      const T* vrow = V + (kp * page_rows + head_row + (j & in_page)) * HD + lg * 4 * VJ;
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int d = 0; d < VJ; ++d) c.o[d][i] += w * to_f(vrow[i * VJ + d]);
+    }
+}
+
+// The natural logarithm of a column's sum of exponentials from its maximum and sum in powers of two.
+__device__ __forceinline__ float lse_of(float m, float l) { return (m + log2f(l)) * 0.6931471805599453f; }
+
+// Sum and exclusive prefix of an integer over the wave's lanes.
+__device__ __forceinline__ int wave_prefix(int v, int& total) {
+  const int lane = threadIdx.x & 63;
+  int x = v;
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    const int y = __shfl_up(x, d);
+    if (lane >= d) x += y;
+  }
+  total = __shfl(x, 63);
+  return x - v;
+}
+
+// ------------------------------------------------------------------ tiles of rows
+// The rows of a request with several, each with the heads that share a key head, are columns: column x is head x % group
+// of row x / group, so that a tile of columns spans few positions.
+struct RowTiles {
+  int n;        // tiles of all requests
+  int b, tile;  // the request of one of them and its number there, -1: there are not so many
+};
+// Tile `at` of all requests, counted from the last one, whose rows see the most keys and that is begun first.
+__device__ __forceinline__ RowTiles row_tiles(const PagedAttnArgs& a, int at) {
+  RowTiles found{0, -1, 0};
+  int b0 = 0;
+  for (; b0 < a.c.n_seq; b0 += 64) {
+    const int b = b0 + (threadIdx.x & 63);
+    int n = 0, all;
+    if (b < a.c.n_seq) {
+      const Request r = request_at(a.c, b);
+      if (r.n > 1) n = (r.n * a.group + a.row_tile - 1) / a.row_tile;
+    }
+    const int prefix = wave_prefix(n, all);
+    // counted from the first one of the chunks so far: every chunk may hold it
+    const unsigned long long past = __ballot(found.n + prefix + n > at);
+    if (found.b < 0 && past) {
+      const int l = __builtin_ctzll(past);
+      found.b = b0 + l;
+      found.tile = __shfl(n, l) - 1 - (at - found.n - __shfl(prefix, l));  // a request's last tile first
+    }
+    found.n += all;
+  }
+  return found;
+}
+
+struct RowTile {
+  Request r;
+  int col0, cols;       // columns [col0, col0 + cols) of the request
+  int lowest, highest;  // positions of the first and the last
+  KeyTiles keys;
+  int splits, per;      // parts that the key tiles are cut into, tiles of a part
+};
+constexpr int SPLIT_TILES = 16;  // key tiles of a part, at least
+__device__ __forceinline__ RowTile row_tile(const PagedAttnArgs& a, const RowTiles& at) {
+  RowTile t;
+  t.r = request_at(a.c, at.b);
+  t.col0 = at.tile * a.row_tile;
+  t.cols = min(a.row_tile, t.r.n * a.group - t.col0);
+  t.lowest = t.r.len - t.r.n + t.col0 / a.group;
+  t.highest = t.r.len - t.r.n + (t.col0 + t.cols - 1) / a.group;
+  t.keys = key_tiles(a, t.lowest, t.highest);
+  const int most = min(a.row_splits, max(ROW_GRID / (at.n * a.c.n_kv_heads), 1));
+  t.splits = max(min(most, t.keys.n / SPLIT_TILES), 1);
+  t.per = (t.keys.n + t.splits - 1) / t.splits;
+  return t;
+}
+// Partial result of one part: a.row_tile x HD outputs, then a maximum and a sum for each column.
+__device__ __forceinline__ float* row_part(const PagedAttnArgs& a, int hd, int n_tiles, int item, int split) {
+  return a.parts + a.rows_at + ((size_t)split * n_tiles * a.c.n_kv_heads + item) * paged_part_floats(a.row_tile, hd);
+}
+
+}  // namespace af
