@@ -50,7 +50,12 @@ struct PagedAttnArgs {
 };
 // A partial result: outputs of `cols` columns, then a maximum and a sum for each, in whole chunks of 16 bytes.
 __host__ __device__ inline size_t paged_part_floats(int cols, int hd) { return ((size_t)cols * (hd + 2) + 3) / 4 * 4; }
-inline int paged_row_tile(int dtype, int head_dim) { return 64; }  // columns of a tile of rows
+// Tiles of rows: columns and keys of one, which go by the type, and the fewest keys of a part of them.
+template <typename T>
+constexpr int ROW_TILE = sizeof(T) == 2 ? 128 : 64;
+template <typename T>
+constexpr int ROW_KEYS = sizeof(T) == 2 ? 64 : 32;
+constexpr int SPLIT_KEYS = 512;
 constexpr int ROW_GRID = 1024;  // workgroups that a split of tiles of rows is to give
 
 // How a call of these sizes is launched, and its workspace.

@@ -90,9 +90,9 @@ constexpr int DIRECT_KEYS = 512;   // caches of so many keys at most are not spl
 struct Shares {
   int total, per;  // tiles of all requests, of a share
 };
-__device__ __forceinline__ int single_tiles(const PagedAttnArgs& a, int b, KeyTiles& t) {
+__device__ __forceinline__ int single_tiles(const PagedAttnArgs& a, int b, KeyTiles<KEY_TILE>& t) {
   const Request r = request_at(a.c, b);
-  t = key_tiles(a, r.len - 1, r.len - 1);
+  t = key_tiles<KEY_TILE>(a, r.len - 1, r.len - 1);
   return r.n == 1 ? t.n : 0;
 }
 // The first request with tiles past tile `at`, and the tiles before it; also their number in all.  Whole waves.
@@ -100,7 +100,7 @@ __device__ __forceinline__ int find_tile(const PagedAttnArgs& a, int at, int& be
   int found = -1, sum = 0;
   for (int b0 = 0; b0 < a.c.n_seq; b0 += 64) {
     const int b = b0 + (threadIdx.x & 63);
-    KeyTiles t;
+    KeyTiles<KEY_TILE> t;
     const int n = b < a.c.n_seq ? single_tiles(a, b, t) : 0;
     int all;
     const int prefix = wave_prefix(n, all);
@@ -146,7 +146,7 @@ __global__ __launch_bounds__(256, 2) void attend_single_kernel(PagedAttnArgs a) 
   }
   for (;;) {
     b = __builtin_amdgcn_readfirstlane(b);
-    KeyTiles t;
+    KeyTiles<KEY_TILE> t;
     const int n = single_tiles(a, b, t);
     const Request r = request_at(a.c, b);
     if (n == 0 && (a.shares || r.n != 1)) {  // (a row without keys: the join writes it)
@@ -159,10 +159,10 @@ __global__ __launch_bounds__(256, 2) void attend_single_kernel(PagedAttnArgs a) 
     c.clear();
     c.load_q(lr < cols ? (const T*)a.q + r.first * a.q_stride + (hk * a.group + col0 + lr) * HD : nullptr);
     int i = i0 + wave;
-    int page = i < i1 ? page_of(a.c, b, t.key(i)) : -1;
+    int page = i < i1 ? page_of<KEY_TILE>(a.c, b, t.key(i)) : -1;
     for (; i < i1; i += SINGLE_WAVES) {
       const int now = page;
-      if (i + SINGLE_WAVES < i1) page = page_of(a.c, b, t.key(i + SINGLE_WAVES));
+      if (i + SINGLE_WAVES < i1) page = page_of<KEY_TILE>(a.c, b, t.key(i + SINGLE_WAVES));
       attend_tile<T, HD, false>(a, hk, t.key(i), now, p, p, p, c);
     }
     // ---- the waves' results, merged
@@ -226,7 +226,7 @@ __device__ __forceinline__ void join_single(const PagedAttnArgs& a, int b, int h
   __shared__ float red[2][4];
   const int tid = threadIdx.x, wave = tid >> 6;
   const Request r = request_at(a.c, b);
-  KeyTiles t;
+  KeyTiles<KEY_TILE> t;
   const int tiles = single_tiles(a, b, t);
   if (r.n != 1) return;
   T* dst = (T*)a.o + r.first * a.o_stride + head * HD;
@@ -285,7 +285,7 @@ __device__ __forceinline__ void join_rows(const PagedAttnArgs& a, int item, int 
   constexpr int DT = HD / 16;
   const RowTiles all = row_tiles(a, item / a.c.n_kv_heads);
   if (all.b < 0) return;
-  const RowTile t = row_tile(a, all);
+  const RowTile<ROW_KEYS<T>> t = row_tile<ROW_KEYS<T>>(a, all);
   const int n = t.splits;
   const int col = col_block * 16 + threadIdx.x / 16, d = threadIdx.x % 16 * DT;
   if (n == 1 || col >= t.cols) return;
@@ -335,12 +335,12 @@ bool paged_plan(int dtype, int head_dim, int n_kv_heads, int n_heads, int n_seq,
     floats = shares * head_blocks * 2 * paged_part_floats(std::min(group, 16), head_dim);
   }
   p->rows_at = floats;
-  p->row_tile = paged_row_tile(dtype, head_dim);
+  p->row_tile = dtype == AF_BF16 ? ROW_TILE<bf16> : ROW_TILE<float>;
   p->row_splits = 1;
   if (!single) {
     const long columns = (long)M * group, tiles = columns / p->row_tile + std::min(n_seq, M / 2);  // at most so many
     row_grid = tiles * n_kv_heads;
-    const long splits = std::min(most_tiles / SPLIT_TILES, (long)ROW_GRID);
+    const long splits = std::min((long)cap / SPLIT_KEYS + 1, (long)ROW_GRID);
     // requests with a single row take n_seq rows at most; what is left may fill the GPU whatever the lengths are
     const long sure = (long)std::max(M - n_seq, 0) * group / p->row_tile * n_kv_heads;
     if (splits > 1 && sure <= ROW_GRID / 2) {

@@ -36,31 +36,45 @@ __device__ __forceinline__ int request_of_row(const PagedCache& c, int row) {
   return -1;
 }
 
-// Keys that positions lowest .. highest can see: [0, sink_end) and [lo, end), as tiles of KEY_TILE keys.
+// Keys that positions lowest .. highest can see: [0, sink_end) and [lo, end), as tiles of TK keys.
 // Tiles 0 .. n_sink - 1 are those of the first keys, the others lie from key tile `first` on; where the two
 // would meet there are no separate first ones.
+template <int TK>
 struct KeyTiles {
   int n_sink, first, n;
-  __device__ __forceinline__ int key(int i) const { return (i < n_sink ? i : first + i - n_sink) * KEY_TILE; }
+  __device__ __forceinline__ int key(int i) const { return (i < n_sink ? i : first + i - n_sink) * TK; }
 };
-__device__ __forceinline__ KeyTiles key_tiles(const PagedAttnArgs& a, int lowest, int highest) {
+template <int TK>
+__device__ __forceinline__ KeyTiles<TK> key_tiles(const PagedAttnArgs& a, int lowest, int highest) {
   const int end = min(highest, a.c.cap - 1) + 1;  // a position of -1 or less sees nothing
   const int lo = min(max(max(lowest, -1) - a.window + 1, 0), max(end, 0));
-  KeyTiles t;
-  t.first = lo / KEY_TILE;
-  t.n_sink = (min(a.sinks, lo) + KEY_TILE - 1) / KEY_TILE;
+  KeyTiles<TK> t;
+  t.first = lo / TK;
+  t.n_sink = (min(a.sinks, lo) + TK - 1) / TK;
   if (t.n_sink >= t.first) t.n_sink = t.first = 0;
-  t.n = end <= 0 ? 0 : t.n_sink + (end + KEY_TILE - 1) / KEY_TILE - t.first;
+  t.n = end <= 0 ? 0 : t.n_sink + (end + TK - 1) / TK - t.first;
   return t;
 }
 // (The clamp keeps p - window within 32 bits where there is none.)
 __device__ __forceinline__ bool sees(const PagedAttnArgs& a, int p, int j) {
   return j <= p && j < a.c.cap && (j > max(p, -1) - a.window || j < a.sinks);
 }
+// Whether some, or all, of the positions lowest .. highest see a key, or every one of n keys from j0 on.
+__device__ __forceinline__ bool some_see(const PagedAttnArgs& a, int lowest, int highest, int j) {
+  return j <= highest && j < a.c.cap && (j > max(lowest, -1) - a.window || j < a.sinks);
+}
+__device__ __forceinline__ bool all_see(const PagedAttnArgs& a, int lowest, int highest, int j0, int n) {
+  return j0 + n - 1 <= lowest && j0 + n <= a.c.cap && (j0 > max(highest, -1) - a.window || j0 + n <= a.sinks);
+}
+// Whether none of them sees one of the n keys.
+__device__ __forceinline__ bool none_see(const PagedAttnArgs& a, int lowest, int highest, int j0, int n) {
+  return j0 > highest || j0 >= a.c.cap || (j0 + n - 1 <= max(lowest, -1) - a.window && j0 >= a.sinks);
+}
 
-// The page of key j0 + lane % 32, -1 where there is none.
+// The page of key j0 + lane % N, -1 where there is none.
+template <int N>
 __device__ __forceinline__ int page_of(const PagedCache& c, int b, int j0) {
-  const int j = j0 + (threadIdx.x & 31);
+  const int j = j0 + (threadIdx.x & (N - 1));
   const int at = j >> c.page_shift;
   const int page = c.table[(size_t)b * c.max_pages + min(at, c.max_pages - 1)];
   return at < c.max_pages && page >= 0 && page < c.n_pages ? page : -1;
@@ -149,8 +163,7 @@ __device__ __forceinline__ void attend_tile(const PagedAttnArgs& a, int hk, int 
 #pragma unroll
     for (int i = 0; i < 4; ++i) s[h * 4 + i] = acc[i] * a.scale_log2;
   }
-  const bool whole = sees(a, lowest, j0 + KEY_TILE - 1) && (j0 > max(highest, -1) - a.window || j0 + KEY_TILE <= a.sinks) &&
-                     __all(page >= 0);
+  const bool whole = all_see(a, lowest, highest, j0, KEY_TILE) && __all(page >= 0);
   bool one_by_one = false;
   if (!whole) {
 #pragma unroll
@@ -158,8 +171,7 @@ __device__ __forceinline__ void attend_tile(const PagedAttnArgs& a, int hk, int 
       const int j = j0 + (e >> 2) * 16 + lg * 4 + (e & 3);
       const bool there = of_page[e >> 2] >= 0;
       if (!there || !sees(a, p, j)) s[e] = -INFINITY;
-      const bool some = MANY ? there && j <= highest && j < a.c.cap && (j > max(lowest, -1) - a.window || j < a.sinks)
-                             : there && sees(a, p, j);
+      const bool some = there && some_see(a, lowest, highest, j);
 #pragma unroll
       for (int d = 0; d < VJ; ++d) {
         if (!some) v[e][d] = from_f<T>(0.f);
@@ -265,24 +277,25 @@ __device__ __forceinline__ RowTiles row_tiles(const PagedAttnArgs& a, int at) {
   return found;
 }
 
+template <int TK>
 struct RowTile {
   Request r;
   int col0, cols;       // columns [col0, col0 + cols) of the request
   int lowest, highest;  // positions of the first and the last
-  KeyTiles keys;
+  KeyTiles<TK> keys;
   int splits, per;      // parts that the key tiles are cut into, tiles of a part
 };
-constexpr int SPLIT_TILES = 16;  // key tiles of a part, at least
-__device__ __forceinline__ RowTile row_tile(const PagedAttnArgs& a, const RowTiles& at) {
-  RowTile t;
+template <int TK>
+__device__ __forceinline__ RowTile<TK> row_tile(const PagedAttnArgs& a, const RowTiles& at) {
+  RowTile<TK> t;
   t.r = request_at(a.c, at.b);
   t.col0 = at.tile * a.row_tile;
   t.cols = min(a.row_tile, t.r.n * a.group - t.col0);
   t.lowest = t.r.len - t.r.n + t.col0 / a.group;
   t.highest = t.r.len - t.r.n + (t.col0 + t.cols - 1) / a.group;
-  t.keys = key_tiles(a, t.lowest, t.highest);
+  t.keys = key_tiles<TK>(a, t.lowest, t.highest);
   const int most = min(a.row_splits, max(ROW_GRID / (at.n * a.c.n_kv_heads), 1));
-  t.splits = max(min(most, t.keys.n / SPLIT_TILES), 1);
+  t.splits = max(min(most, t.keys.n * TK / SPLIT_KEYS), 1);
   t.per = (t.keys.n + t.splits - 1) / t.splits;
   return t;
 }

@@ -3,18 +3,294 @@
 
 namespace af {
 
-// Four waves, 16 columns each.
-template <typename T, int HD>
+typedef __attribute__((__vector_size__(4 * sizeof(short)))) short s16x4;
+
+__device__ __forceinline__ const char* uniform(const void* p) {
+  const unsigned lo = __builtin_amdgcn_readfirstlane((unsigned)(uintptr_t)p);
+  const unsigned hi = __builtin_amdgcn_readfirstlane((unsigned)((uintptr_t)p >> 32));
+  return (const char*)((uintptr_t)hi << 32 | lo);
+}
+__device__ __forceinline__ float max_of_halves(float v) {  // of lane % 32 and lane % 32 + 32
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+
+// Tiles of 64 keys of a page pool in LDS, keys and values as they lie in the pages: rows of HD elements, the 16-byte
+// chunk c of row r at place c ^ turn(r) of the row.  With that the 16 rows of one access step of a key operand (the same
+// chunk of each) and the 8 rows x 64 bytes of a value operand are spread evenly over the banks.
+template <int HD>
+struct PageTiles {
+  static constexpr int KEYS = ROW_KEYS<bf16>, ROW = HD * 2, CHUNKS = HD / 8;
+  static constexpr int BYTES = KEYS * ROW, STAGE = 2 * BYTES;
+  static constexpr int STEP = 64 / CHUNKS;                // rows that a wave's load fills
+  static constexpr int LOADS = KEYS / STEP / 4;           // loads of a wave for a tile of keys, and of values
+  static_assert(STEP <= PAGED_MIN_PAGE && KEYS % (STEP * 4) == 0, "a load's rows lie in one page");
+  __device__ __forceinline__ static int turn(int r) {
+    if constexpr (HD == 128) return (r & 3) << 2 | (r >> 2 & 3);
+    else return (r >> 1 & 1) << 2 | (r >> 2 & 3);
+  }
+};
+
+// bf16.  Four waves of 32 columns each; the tiles of 64 keys go to LDS without passing registers, the next one while
+// this one is worked on.  Scores, and outputs, are taken transposed as in Columns: S^T = K . Q^T and O^T = V^T . P^T on
+// 32 x 32 tiles, so that a lane holds (half of) one column alone.  The probabilities are the second product's operand
+// as they are: a lane has keys 8 i + 4 h + 0..3 (h = lane / 32), and the values' operand is read in that order, by
+// LDS reads that transpose 4 x 16 elements.
+// Outputs are scaled to a new maximum only when it passes the old one by 2^8 in some column: until then
+// probabilities go up to 2^8 instead of 1, with the same relative precision.
+// A probability is rounded to bf16 once (2^-8 of it at most): a remainder as in attend_tile would cost a third
+// more matrix instructions, which bound this kernel.  Sums are of the unrounded ones.
+template <int HD>
+__global__ __launch_bounds__(256, 2) void attend_tiles_kernel(PagedAttnArgs a) {
+  typedef PageTiles<HD> L;
+  constexpr int TK = L::KEYS, KST = HD / 16, OB = HD / 32;
+  __shared__ __attribute__((aligned(1024))) char smem[2 * L::STAGE];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), ln = lane & 31, h = lane >> 5;
+  const int hk = blockIdx.x % a.c.n_kv_heads;
+  RowTiles at = row_tiles(a, 0x7fffffff);
+  if (at.n == 0) return;
+  const int split = blockIdx.x / a.c.n_kv_heads / at.n, item = blockIdx.x / a.c.n_kv_heads % at.n;
+  at = row_tiles(a, item);
+  const RowTile<TK> t = row_tile<TK>(a, at);
+  if (split >= t.splits) return;
+
+  // ---- the wave's columns (those past the last one repeat it and are not stored)
+  const int w0 = wave * 32;
+  const bool busy = w0 < t.cols;
+  const int col = t.col0 + min(w0 + ln, t.cols - 1);
+  const int row = t.r.first + col / a.group, head = hk * a.group + col % a.group;
+  const int base = t.r.len - t.r.n, p = base + col / a.group;
+  const int lowest = base + (t.col0 + min(w0, t.cols - 1)) / a.group, highest = base + (t.col0 + min(w0 + 31, t.cols - 1)) / a.group;
+  // a scale below 0 turns the queries' sign, and one of 0 clears them, so that the largest score has the largest product
+  const float sign = a.scale_log2 > 0.f ? 1.f : a.scale_log2 < 0.f ? -1.f : 0.f;
+  const float sl = a.scale_log2 == 0.f ? 1.f : fabsf(a.scale_log2);
+  bf16x8 q[KST];
+  {
+    const bf16* src = (const bf16*)a.q + row * a.q_stride + head * HD + h * 8;
+#pragma unroll
+    for (int s = 0; s < KST; ++s) {
+      q[s] = *(const bf16x8*)(src + s * 16);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) q[s][e] = (bf16)((float)q[s][e] * sign);
+    }
+  }
+
+  // ---- loads: row `step row` + lane / CHUNKS of the tile, its chunk (lane % CHUNKS) ^ turn(row)
+  const unsigned lds0 = __builtin_amdgcn_readfirstlane((unsigned)(uintptr_t)(__attribute__((address_space(3))) char*)smem);
+  unsigned voff[L::LOADS];
+#pragma unroll
+  for (int i = 0; i < L::LOADS; ++i) {
+    const int r = (wave * L::LOADS + i) * L::STEP + lane / L::CHUNKS;
+    voff[i] = lane / L::CHUNKS * L::ROW + (lane % L::CHUNKS ^ L::turn(r)) * 16;
+  }
+  const int in_page = (1 << a.c.page_shift) - 1;
+  const auto load = [&](int j0, int pages, int buf) {  // pages: of key j0 + lane
+#pragma unroll
+    for (int i = 0; i < L::LOADS; ++i) {
+      const int r = (wave * L::LOADS + i) * L::STEP;
+      const int page = max(__builtin_amdgcn_readlane(pages, r), 0);
+      const size_t at = ((((size_t)page * a.c.n_kv_heads + hk) << a.c.page_shift) + ((j0 + r) & in_page)) * L::ROW;
+      dma16(uniform((const char*)a.c.k + at), voff[i], lds0 + buf * L::STAGE + r * L::ROW);
+      dma16(uniform((const char*)a.c.v + at), voff[i], lds0 + buf * L::STAGE + L::BYTES + r * L::ROW);
+    }
+  };
+
+  // ---- LDS addresses: key ln of a block of 32, chunk 2 s + h; values 4 h + lane % 16 / 4 (and 8 further) of 16, dimensions
+  // 16 (lane / 16 % 2) + 4 (lane % 4) of 32
+  const int kz = L::turn(ln) ^ h, x = lane & 15, vr = 4 * h + (x >> 2);
+  const int vc = (lane >> 4 & 1) * 2 + (x >> 1 & 1);
+  const int k_at = ln * L::ROW;
+  int v_at[2][OB];
+#pragma unroll
+  for (int i = 0; i < 2; ++i)
+#pragma unroll
+    for (int c = 0; c < OB; ++c) v_at[i][c] = (vr + 8 * i) * L::ROW + ((4 * c) ^ (vc ^ L::turn(vr + 8 * i))) * 16 + (x & 1) * 8;
+
+  f32x16 o[OB];
+#pragma unroll
+  for (int c = 0; c < OB; ++c)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) o[c][e] = 0.f;
+  float m = -INFINITY, l = 0.f;
+
+  int i = split * t.per;
+  const int end = min(i + t.per, t.keys.n);
+  int pages = -1, next_pages = -1;
+  if (i < end) {
+    pages = page_of<TK>(a.c, at.b, t.keys.key(i));
+    load(t.keys.key(i), pages, 0);
+    if (i + 1 < end) next_pages = page_of<TK>(a.c, at.b, t.keys.key(i + 1));
+  }
+  for (int buf = 0; i < end; ++i, buf ^= 1) {
+    const int j0 = t.keys.key(i);
+    // this tile is there, and every wave is done with the other one
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    const unsigned long long there = __ballot(pages >= 0);
+    pages = next_pages;
+    if (i + 1 < end) load(t.keys.key(i + 1), pages, buf ^ 1);
+    if (i + 2 < end) next_pages = page_of<TK>(a.c, at.b, t.keys.key(i + 2));
+    const char* Kt = smem + buf * L::STAGE;
+    char* Vt = smem + buf * L::STAGE + L::BYTES;
+
+    // ---- tiles that some column does not see whole: values that nobody sees become zeros, since a probability of 0 does
+    // not hide an infinity or a NaN; where others are not finite, products are taken one by one
+    bool one_by_one = false;
+    if (!(all_see(a, t.lowest, t.highest, j0, TK) && there == ~0ull)) {
+      constexpr int T = 256 / TK, N = L::CHUNKS / T;  // threads of a row, chunks of each
+      const int r = tid / T;
+      const bool some = (there >> r & 1) && some_see(a, t.lowest, t.highest, j0 + r);
+      bool odd = false;
+#pragma unroll
+      for (int c = 0; c < N; ++c) {
+        uint4* at16 = (uint4*)(Vt + r * L::ROW + (tid % T * N + c) * 16);
+        if (some) {
+          const uint4 w = *at16;
+          const unsigned u[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+          for (int e = 0; e < 4; ++e) odd |= (u[e] & 0x7f80u) == 0x7f80u || (u[e] & 0x7f800000u) == 0x7f800000u;
+        } else {
+          *at16 = zero4();
+        }
+      }
+      one_by_one = __syncthreads_or(odd);
+    }
+    const bool seen = busy && !none_see(a, lowest, highest, j0, TK);
+    const bool whole = all_see(a, lowest, highest, j0, TK) && there == ~0ull;
+
+    f32x16 s[2];
+    bf16x8 pf[4];
+    if (seen) {
+      // ---- S^T = K . Q^T
+#pragma unroll
+      for (int b = 0; b < 2; ++b) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) s[b][e] = 0.f;
+#pragma unroll
+        for (int c = 0; c < KST; ++c) {
+          const bf16x8 kf = *(const bf16x8*)(Kt + k_at + b * 32 * L::ROW + ((2 * c) ^ kz) * 16);
+          s[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, q[c], s[b], 0, 0, 0);
+        }
+      }
+      if (!whole) {
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) {
+            const int k = b * 32 + 8 * (e >> 2) + 4 * h + (e & 3);
+            if (!(there >> k & 1) || !sees(a, p, j0 + k)) s[b][e] = -INFINITY;
+          }
+      }
+      // ---- softmax
+      float top = s[0][0];
+#pragma unroll
+      for (int b = 0; b < 2; ++b)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) top = fmaxf(top, s[b][e]);
+      top = max_of_halves(top);
+      if (__any((top - m) * sl > 8.f)) {
+        const float up = fmaxf(m, top), ref = up == -INFINITY ? 0.f : up;
+        const float f = __builtin_amdgcn_exp2f((m - ref) * sl);
+        l *= f;
+#pragma unroll
+        for (int c = 0; c < OB; ++c) o[c] *= f;
+        m = up;
+      }
+      const float off = m == -INFINITY ? 0.f : m * sl;  // no key seen yet: the probabilities come out 0
+#pragma unroll
+      for (int b = 0; b < 2; ++b)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          s[b][e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][e], sl, -off));
+          l += s[b][e];
+          pf[b * 2 + (e >> 3)][e & 7] = (bf16)s[b][e];
+        }
+    }
+    if (!one_by_one) {
+      // ---- O^T += V^T . P^T
+      if (seen) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+#pragma unroll
+          for (int c = 0; c < OB; ++c) {
+            typedef __attribute__((address_space(3))) s16x4 lds4;
+            const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4*)(Vt + v_at[0][c] + k * 16 * L::ROW));
+            const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4*)(Vt + v_at[1][c] + k * 16 * L::ROW));
+            bf16x8 vf;
+            __builtin_memcpy(&vf, &lo, 8);
+            __builtin_memcpy((char*)&vf + 8, &hi, 8);
+            o[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pf[k], o[c], 0, 0, 0);
+          }
+      }
+    } else {
+      __syncthreads();  // the keys are done with: a wave's part of them takes its probabilities, 32 keys at a time
+      bf16* mine = (bf16*)(Kt + wave * (L::BYTES / 4));
+      for (int b = 0; b < 2 && seen; ++b) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) mine[(8 * (e >> 2) + 4 * h + (e & 3)) * 32 + ln] = (bf16)(b ? s[1][e] : s[0][e]);
+        __builtin_amdgcn_wave_barrier();
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+#pragma unroll 1
+        for (int k = 0; k < 32; ++k) {
+          const int r = b * 32 + k;
+          if (!(there >> r & 1) || !sees(a, p, j0 + r)) continue;
+          const float w = (float)mine[k * 32 + ln];
+#pragma unroll
+          for (int c = 0; c < OB; ++c)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+              const int d = 32 * c + 8 * (e >> 2) + 4 * h + (e & 3);
+              o[c][e] += w * (float)*(const bf16*)(Vt + r * L::ROW + ((d / 8) ^ L::turn(r)) * 16 + d % 8 * 2);
+            }
+        }
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+      }
+    }
+  }
+
+  if (!busy) return;
+  l += __shfl_xor(l, 32);
+  if (w0 + ln >= t.cols) return;
+  if (t.splits == 1) {
+    const float inv = l == 0.f ? 0.f : 1.0f / l;
+    bf16* dst = (bf16*)a.o + row * a.o_stride + head * HD + 4 * h;
+#pragma unroll
+    for (int c = 0; c < OB; ++c)
+#pragma unroll
+      for (int b = 0; b < 4; ++b) {
+        bf16x4 w;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) w[e] = (bf16)(o[c][4 * b + e] * inv);
+        *(bf16x4*)(dst + 32 * c + 8 * b) = w;
+      }
+    if (a.lse && h == 0) a.lse[(size_t)row * a.n_heads + head] = lse_of(m * sl, l);
+  } else {
+    float* part = row_part(a, HD, at.n, item * a.c.n_kv_heads + hk, split);
+#pragma unroll
+    for (int c = 0; c < OB; ++c)
+#pragma unroll
+      for (int b = 0; b < 4; ++b)
+        *(f32x4*)(part + (w0 + ln) * HD + 32 * c + 8 * b + 4 * h) = f32x4{o[c][4 * b], o[c][4 * b + 1], o[c][4 * b + 2], o[c][4 * b + 3]};
+    if (h == 0) {
+      part[a.row_tile * HD + 2 * (w0 + ln)] = m * sl;
+      part[a.row_tile * HD + 2 * (w0 + ln) + 1] = l;
+    }
+  }
+}
+
+// fp32.  Four waves, 16 columns each, that read keys and values themselves: the matrix instructions of this
+// type, a sixteenth as fast, bound it.
+template <int HD>
 __global__ __launch_bounds__(256, 2) void attend_rows_kernel(PagedAttnArgs a) {
-  typedef Columns<T, HD> C;
-  constexpr int VJ = C::VJ;
+  typedef Columns<float, HD> C;
+  constexpr int VJ = C::VJ, TK = KEY_TILE;
+  static_assert(ROW_KEYS<float> == KEY_TILE && ROW_TILE<float> == 64, "four waves of 16 columns");
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, lr = lane & 15, lg = lane >> 4;
   const int hk = blockIdx.x % a.c.n_kv_heads;
   RowTiles at = row_tiles(a, 0x7fffffff);
   if (at.n == 0) return;
   const int split = blockIdx.x / a.c.n_kv_heads / at.n, item = blockIdx.x / a.c.n_kv_heads % at.n;
   at = row_tiles(a, item);
-  const RowTile t = row_tile(a, at);
+  const RowTile<TK> t = row_tile<TK>(a, at);
   if (split >= t.splits) return;
   const int w0 = wave * 16;
   if (w0 >= t.cols) return;
@@ -24,22 +300,22 @@ __global__ __launch_bounds__(256, 2) void attend_rows_kernel(PagedAttnArgs a) {
   const int lowest = base + (t.col0 + w0) / a.group, highest = base + (t.col0 + min(w0 + 15, t.cols - 1)) / a.group;
   C c;
   c.clear();
-  c.load_q((const T*)a.q + row * a.q_stride + head * HD);
+  c.load_q((const float*)a.q + row * a.q_stride + head * HD);
   const int end = min((split + 1) * t.per, t.keys.n);
   for (int i = split * t.per; i < end; ++i) {
     const int j0 = t.keys.key(i);
-    if (j0 > highest || (j0 + KEY_TILE - 1 <= max(lowest, -1) - a.window && j0 >= a.sinks)) continue;
-    attend_tile<T, HD, true>(a, hk, j0, page_of(a.c, at.b, j0), p, lowest, highest, c);
+    if (none_see(a, lowest, highest, j0, TK)) continue;
+    attend_tile<float, HD, true>(a, hk, j0, page_of<TK>(a.c, at.b, j0), p, lowest, highest, c);
   }
   const float l = c.sum();
   if (w0 + lr >= t.cols) return;
   if (t.splits == 1) {
     const float inv = l == 0.f ? 0.f : 1.0f / l;
-    T* dst = (T*)a.o + row * a.o_stride + head * HD + lg * 4 * VJ;
+    float* dst = (float*)a.o + row * a.o_stride + head * HD + lg * 4 * VJ;
 #pragma unroll
     for (int e = 0; e < 4; ++e)
 #pragma unroll
-      for (int j = 0; j < VJ; ++j) dst[e * VJ + j] = from_f<T>(c.o[j][e] * inv);
+      for (int j = 0; j < VJ; ++j) dst[e * VJ + j] = c.o[j][e] * inv;
     if (a.lse && lg == 0) a.lse[(size_t)row * a.n_heads + head] = lse_of(c.m, l);
   } else {
     float* part = row_part(a, HD, at.n, item * a.c.n_kv_heads + hk, split);
@@ -56,11 +332,11 @@ __global__ __launch_bounds__(256, 2) void attend_rows_kernel(PagedAttnArgs a) {
 
 hipError_t launch_paged_rows(int dtype, int head_dim, const PagedAttnArgs& a, int grid, hipStream_t s) {
   if (dtype == AF_BF16) {
-    if (head_dim == 128) hipLaunchKernelGGL((attend_rows_kernel<bf16, 128>), dim3(grid), dim3(256), 0, s, a);
-    else hipLaunchKernelGGL((attend_rows_kernel<bf16, 64>), dim3(grid), dim3(256), 0, s, a);
+    if (head_dim == 128) hipLaunchKernelGGL((attend_tiles_kernel<128>), dim3(grid), dim3(256), 0, s, a);
+    else hipLaunchKernelGGL((attend_tiles_kernel<64>), dim3(grid), dim3(256), 0, s, a);
   } else {
-    if (head_dim == 128) hipLaunchKernelGGL((attend_rows_kernel<float, 128>), dim3(grid), dim3(256), 0, s, a);
-    else hipLaunchKernelGGL((attend_rows_kernel<float, 64>), dim3(grid), dim3(256), 0, s, a);
+    if (head_dim == 128) hipLaunchKernelGGL((attend_rows_kernel<128>), dim3(grid), dim3(256), 0, s, a);
+    else hipLaunchKernelGGL((attend_rows_kernel<64>), dim3(grid), dim3(256), 0, s, a);
   }
   return hipGetLastError();
 }

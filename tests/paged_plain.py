@@ -85,21 +85,23 @@ class Step:
         return out
 
     # ------------------------------------------------------------------ attention
-    def attended(self, scale, window=0, sinks=0, p_bits=2.0 ** -16):
+    def attended(self, scale, window=0, sinks=0):
         """(o, its bound, lse, its bound) in 64 bits for every row; rows of no request are NaN.
 
         A score is a product of hd exact terms summed in fp32, and scaled: off by (hd + 3) U32 of the sum of their
         magnitudes; its distance to the maximum is rounded once more.  exp2 is within an ulp (2^-23).  A weight is
-        held to p_bits (bf16) or exactly (fp32).  n weights, and their products with values, are summed in fp32, in
-        any order: n U32.  The error of a weight counts in the numerator and in the denominator."""
+        multiplied with values as it is (fp32), as a bf16 number and a bf16 remainder (bf16, requests with a single row:
+        2^-8 of 2^-8 is lost) or as a bf16 number (bf16, several rows: half a step, 2^-8).  n weights, and their products
+        with values, are summed in fp32, in any order: n U32.  A weight's error counts in the numerator and in the
+        denominator, but for its rounding to bf16, which the sum of weights does not have."""
         o = torch.full((self.M, self.Hq, self.hd), math.nan, dtype=torch.float64)
         o_bound, lse = torch.full_like(o, math.nan), torch.full((self.M, self.Hq), math.nan, dtype=torch.float64)
         lse_bound = torch.full_like(lse, math.nan)
         kc, vc = self.k_cache.double(), self.v_cache.double()
-        held = 0.0 if self.dtype is torch.float32 else p_bits
         for b, (n, length) in enumerate(self.requests):
             if n == 0:
                 continue
+            held = 0.0 if self.dtype is torch.float32 else 2.0 ** -16 if n == 1 else 2.0 ** -8
             keys = [j for j in range(max(length, 0)) if self.cell(b, j) is not None]
             cells = [self.cell(b, j) for j in keys]
             pg, off = torch.tensor([c[0] for c in cells], dtype=torch.long), torch.tensor([c[1] for c in cells], dtype=torch.long)
@@ -120,10 +122,10 @@ class Step:
                 w = torch.softmax(s, dim=2)
                 far = (s.amax(dim=2, keepdim=True) - s) * U32
                 each = (self.hd + 3) * U32 * size + far + 2.0 ** -23
-                worst = each.amax(dim=2, keepdim=True) + held + see.sum() * U32
+                worst = each.amax(dim=2, keepdim=True) + see.sum() * U32
                 r = torch.einsum("hgk,khd->hgd", w, v)
                 total = torch.einsum("hgk,khd->hgd", w, v.abs())
-                err = 2 * worst * total
+                err = (2 * worst + held) * total
                 o[row] = r.reshape(self.Hq, self.hd)
                 o_bound[row] = (err + HALF_STEP[self.dtype] * (r.abs() + err)).reshape(self.Hq, self.hd)
                 top = torch.logsumexp(s, dim=2)
