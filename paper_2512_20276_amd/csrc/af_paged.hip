@@ -283,19 +283,18 @@ __device__ __forceinline__ void join_single(const PagedAttnArgs& a, int b, int h
 template <typename T, int HD>
 __device__ __forceinline__ void join_rows(const PagedAttnArgs& a, int item, int col_block) {
   constexpr int DT = HD / 16;
-  const RowTiles all = row_tiles(a, item / a.c.n_kv_heads);
-  if (all.b < 0) return;
-  const RowTile<ROW_KEYS<T>> t = row_tile<ROW_KEYS<T>>(a, all);
+  const RowTile<ROW_KEYS<T>> t = row_tile<ROW_KEYS<T>>(a, item / a.c.n_kv_heads);
+  if (t.b < 0 || t.split > 0) return;
   const int n = t.splits;
   const int col = col_block * 16 + threadIdx.x / 16, d = threadIdx.x % 16 * DT;
   if (n == 1 || col >= t.cols) return;
   const int hk = item % a.c.n_kv_heads;
   float m = -INFINITY, l = 0.f;
-  for (int i = 0; i < n; ++i) m = fmaxf(m, row_part(a, HD, all.n, item, i)[a.row_tile * HD + 2 * col]);
+  for (int i = 0; i < n; ++i) m = fmaxf(m, row_part(a, HD, t.n, item, i)[a.row_tile * HD + 2 * col]);
   const float ref = m == -INFINITY ? 0.f : m;
   float o[DT] = {};
   for (int i = 0; i < n; ++i) {
-    const float* part = row_part(a, HD, all.n, item, i);
+    const float* part = row_part(a, HD, t.n, item, i);
     const float f = exp2f(part[a.row_tile * HD + 2 * col] - ref);
     l += f * part[a.row_tile * HD + 2 * col + 1];
 #pragma unroll

@@ -249,54 +249,62 @@ __device__ __forceinline__ int wave_prefix(int v, int& total) {
 // ------------------------------------------------------------------ tiles of rows
 // The rows of a request with several, each with the heads that share a key head, are columns: column x is head x % group
 // of row x / group, so that a tile of columns spans few positions.
-struct RowTiles {
-  int n;        // tiles of all requests
-  int b, tile;  // the request of one of them and its number there, -1: there are not so many
-};
-// Tile `at` of all requests, counted from the last one, whose rows see the most keys and that is begun first.
-__device__ __forceinline__ RowTiles row_tiles(const PagedAttnArgs& a, int at) {
-  RowTiles found{0, -1, 0};
-  int b0 = 0;
-  for (; b0 < a.c.n_seq; b0 += 64) {
-    const int b = b0 + (threadIdx.x & 63);
-    int n = 0, all;
-    if (b < a.c.n_seq) {
-      const Request r = request_at(a.c, b);
-      if (r.n > 1) n = (r.n * a.group + a.row_tile - 1) / a.row_tile;
-    }
-    const int prefix = wave_prefix(n, all);
-    // counted from the first one of the chunks so far: every chunk may hold it
-    const unsigned long long past = __ballot(found.n + prefix + n > at);
-    if (found.b < 0 && past) {
-      const int l = __builtin_ctzll(past);
-      found.b = b0 + l;
-      found.tile = __shfl(n, l) - 1 - (at - found.n - __shfl(prefix, l));  // a request's last tile first
-    }
-    found.n += all;
-  }
-  return found;
-}
-
+// A workgroup takes a part of the keys of one tile of columns.
 template <int TK>
 struct RowTile {
+  int b;                // the request, -1: nothing to do
+  int n, item, split;   // tiles of all requests, the one that is taken, the part of its keys
   Request r;
   int col0, cols;       // columns [col0, col0 + cols) of the request
   int lowest, highest;  // positions of the first and the last
   KeyTiles<TK> keys;
   int splits, per;      // parts that the key tiles are cut into, tiles of a part
 };
+__device__ __forceinline__ int scalar(int v) { return __builtin_amdgcn_readfirstlane(v); }
+// Workgroup `at` of a key head (all parts 0 first).  A request's last tile, whose rows see the most keys, is begun first.
+// The requests are read once by the lanes of a wave, a second time only where they are more than 64.
 template <int TK>
-__device__ __forceinline__ RowTile<TK> row_tile(const PagedAttnArgs& a, const RowTiles& at) {
+__device__ __forceinline__ RowTile<TK> row_tile(const PagedAttnArgs& a, int at) {
+  const int lane = threadIdx.x & 63;
   RowTile<TK> t;
-  t.r = request_at(a.c, at.b);
-  t.col0 = at.tile * a.row_tile;
+  t.b = -1, t.n = 0;
+  Request r{0, 0, 0};
+  int n = 0, prefix = 0, all = 0;
+  const auto read = [&](int b0) {
+    n = 0;
+    if (b0 + lane < a.c.n_seq) {
+      r = request_at(a.c, b0 + lane);
+      if (r.n > 1) n = (r.n * a.group + a.row_tile - 1) / a.row_tile;
+    }
+    prefix = wave_prefix(n, all);
+    all = scalar(all);
+  };
+  for (int b0 = 0; b0 < a.c.n_seq; b0 += 64) {
+    read(b0);
+    t.n += all;
+  }
+  if (t.n == 0) return t;
+  t.item = at % t.n, t.split = at / t.n;
+  for (int b0 = 0, before = 0; b0 < a.c.n_seq; b0 += 64) {
+    if (a.c.n_seq > 64) read(b0);
+    const unsigned long long past = __ballot(before + prefix + n > t.item);
+    if (past) {
+      const int l = __builtin_ctzll(past);
+      t.b = b0 + l;
+      t.r = Request{__builtin_amdgcn_readlane(r.first, l), __builtin_amdgcn_readlane(r.n, l), __builtin_amdgcn_readlane(r.len, l)};
+      t.col0 = (__builtin_amdgcn_readlane(n, l) - 1 - (t.item - before - __builtin_amdgcn_readlane(prefix, l))) * a.row_tile;
+      break;
+    }
+    before += all;
+  }
   t.cols = min(a.row_tile, t.r.n * a.group - t.col0);
   t.lowest = t.r.len - t.r.n + t.col0 / a.group;
   t.highest = t.r.len - t.r.n + (t.col0 + t.cols - 1) / a.group;
   t.keys = key_tiles<TK>(a, t.lowest, t.highest);
-  const int most = min(a.row_splits, max(ROW_GRID / (at.n * a.c.n_kv_heads), 1));
+  const int most = min(a.row_splits, max(ROW_GRID / (t.n * a.c.n_kv_heads), 1));
   t.splits = max(min(most, t.keys.n * TK / SPLIT_KEYS), 1);
   t.per = (t.keys.n + t.splits - 1) / t.splits;
+  if (t.split >= t.splits) t.b = -1;
   return t;
 }
 // Partial result of one part: a.row_tile x HD outputs, then a maximum and a sum for each column.

@@ -47,12 +47,8 @@ __global__ __launch_bounds__(256, 2) void attend_tiles_kernel(PagedAttnArgs a) {
   __shared__ __attribute__((aligned(1024))) char smem[2 * L::STAGE];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), ln = lane & 31, h = lane >> 5;
   const int hk = blockIdx.x % a.c.n_kv_heads;
-  RowTiles at = row_tiles(a, 0x7fffffff);
-  if (at.n == 0) return;
-  const int split = blockIdx.x / a.c.n_kv_heads / at.n, item = blockIdx.x / a.c.n_kv_heads % at.n;
-  at = row_tiles(a, item);
-  const RowTile<TK> t = row_tile<TK>(a, at);
-  if (split >= t.splits) return;
+  const RowTile<TK> t = row_tile<TK>(a, blockIdx.x / a.c.n_kv_heads);
+  if (t.b < 0) return;
 
   // ---- the wave's columns (those past the last one repeat it and are not stored)
   const int w0 = wave * 32;
@@ -113,13 +109,13 @@ __global__ __launch_bounds__(256, 2) void attend_tiles_kernel(PagedAttnArgs a) {
     for (int e = 0; e < 16; ++e) o[c][e] = 0.f;
   float m = -INFINITY, l = 0.f;
 
-  int i = split * t.per;
+  int i = t.split * t.per;
   const int end = min(i + t.per, t.keys.n);
   int pages = -1, next_pages = -1;
   if (i < end) {
-    pages = page_of<TK>(a.c, at.b, t.keys.key(i));
+    pages = page_of<TK>(a.c, t.b, t.keys.key(i));
     load(t.keys.key(i), pages, 0);
-    if (i + 1 < end) next_pages = page_of<TK>(a.c, at.b, t.keys.key(i + 1));
+    if (i + 1 < end) next_pages = page_of<TK>(a.c, t.b, t.keys.key(i + 1));
   }
   for (int buf = 0; i < end; ++i, buf ^= 1) {
     const int j0 = t.keys.key(i);
@@ -128,7 +124,7 @@ __global__ __launch_bounds__(256, 2) void attend_tiles_kernel(PagedAttnArgs a) {
     const unsigned long long there = __ballot(pages >= 0);
     pages = next_pages;
     if (i + 1 < end) load(t.keys.key(i + 1), pages, buf ^ 1);
-    if (i + 2 < end) next_pages = page_of<TK>(a.c, at.b, t.keys.key(i + 2));
+    if (i + 2 < end) next_pages = page_of<TK>(a.c, t.b, t.keys.key(i + 2));
     const char* Kt = smem + buf * L::STAGE;
     char* Vt = smem + buf * L::STAGE + L::BYTES;
 
@@ -160,24 +156,45 @@ __global__ __launch_bounds__(256, 2) void attend_tiles_kernel(PagedAttnArgs a) {
     f32x16 s[2];
     bf16x8 pf[4];
     if (seen) {
-      // ---- S^T = K . Q^T
+      // ---- S^T = K . Q^T, four operands ahead
+      bf16x8 kf[2][4];
+      const auto read = [&](int g) {  // four of the 2 KST operands
 #pragma unroll
-      for (int b = 0; b < 2; ++b) {
+        for (int c = 0; c < 4; ++c)
+          kf[g & 1][c] = *(const bf16x8*)(Kt + k_at + (4 * g + c) / KST * 32 * L::ROW + ((2 * ((4 * g + c) % KST)) ^ kz) * 16);
+      };
+#pragma unroll
+      for (int b = 0; b < 2; ++b)
 #pragma unroll
         for (int e = 0; e < 16; ++e) s[b][e] = 0.f;
+      read(0);
+      __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
+      static_for<0, KST / 2>([&](auto G) {
+        constexpr int g = decltype(G)::value;
+        if constexpr (g + 1 < KST / 2) read(g + 1);
 #pragma unroll
-        for (int c = 0; c < KST; ++c) {
-          const bf16x8 kf = *(const bf16x8*)(Kt + k_at + b * 32 * L::ROW + ((2 * c) ^ kz) * 16);
-          s[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, q[c], s[b], 0, 0, 0);
+        for (int c = 0; c < 4; ++c) {
+          constexpr int b = 4 * g / KST;
+          s[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[g & 1][c], q[(4 * g + c) % KST], s[b], 0, 0, 0);
         }
-      }
+        if constexpr (g + 1 < KST / 2) {
+#pragma unroll
+          for (int c = 0; c < 4; ++c) {
+            __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+          }
+        }
+      });
       if (!whole) {
+        // the lane's keys are 4 h on from constants: seen are those up to `last` that lie behind `left` or before `first`
+        const int last = min(p, a.c.cap - 1) - j0 - 4 * h, left = max(p, -1) - a.window - j0 - 4 * h, first = a.sinks - j0 - 4 * h;
+        const unsigned long long mine = there >> (4 * h);
 #pragma unroll
         for (int b = 0; b < 2; ++b)
 #pragma unroll
           for (int e = 0; e < 16; ++e) {
-            const int k = b * 32 + 8 * (e >> 2) + 4 * h + (e & 3);
-            if (!(there >> k & 1) || !sees(a, p, j0 + k)) s[b][e] = -INFINITY;
+            const int k = b * 32 + 8 * (e >> 2) + (e & 3);
+            if (!(mine >> k & 1) || k > last || (k <= left && k >= first)) s[b][e] = -INFINITY;
           }
       }
       // ---- softmax
@@ -195,38 +212,56 @@ __global__ __launch_bounds__(256, 2) void attend_tiles_kernel(PagedAttnArgs a) {
         for (int c = 0; c < OB; ++c) o[c] *= f;
         m = up;
       }
+      float sum[2] = {0.f, 0.f};
       const float off = m == -INFINITY ? 0.f : m * sl;  // no key seen yet: the probabilities come out 0
 #pragma unroll
       for (int b = 0; b < 2; ++b)
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
           s[b][e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][e], sl, -off));
-          l += s[b][e];
+          sum[e & 1] += s[b][e];
           pf[b * 2 + (e >> 3)][e & 7] = (bf16)s[b][e];
         }
+      l += sum[0] + sum[1];
     }
     if (!one_by_one) {
       // ---- O^T += V^T . P^T
       if (seen) {
-#pragma unroll
-        for (int k = 0; k < 4; ++k)
+        bf16x8 vf[2][OB];
+        const auto read = [&](int k) {
 #pragma unroll
           for (int c = 0; c < OB; ++c) {
             typedef __attribute__((address_space(3))) s16x4 lds4;
             const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4*)(Vt + v_at[0][c] + k * 16 * L::ROW));
             const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4*)(Vt + v_at[1][c] + k * 16 * L::ROW));
-            bf16x8 vf;
-            __builtin_memcpy(&vf, &lo, 8);
-            __builtin_memcpy((char*)&vf + 8, &hi, 8);
-            o[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pf[k], o[c], 0, 0, 0);
+            __builtin_memcpy(&vf[k & 1][c], &lo, 8);
+            __builtin_memcpy((char*)&vf[k & 1][c] + 8, &hi, 8);
           }
+        };
+        read(0);
+        __builtin_amdgcn_sched_group_barrier(0x100, 2 * OB, 1);
+        static_for<0, 4>([&](auto K) {
+          constexpr int k = decltype(K)::value;
+          if constexpr (k < 3) read(k + 1);
+#pragma unroll
+          for (int c = 0; c < OB; ++c) o[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[k & 1][c], pf[k], o[c], 0, 0, 0);
+          if constexpr (k < 3) {
+#pragma unroll
+            for (int c = 0; c < OB; ++c) {
+              __builtin_amdgcn_sched_group_barrier(0x100, 2, 1);
+              __builtin_amdgcn_sched_group_barrier(0x8, 1, 1);
+            }
+          }
+        });
       }
     } else {
       __syncthreads();  // the keys are done with: a wave's part of them takes its probabilities, 32 keys at a time
       bf16* mine = (bf16*)(Kt + wave * (L::BYTES / 4));
-      for (int b = 0; b < 2 && seen; ++b) {
 #pragma unroll
-        for (int e = 0; e < 16; ++e) mine[(8 * (e >> 2) + 4 * h + (e & 3)) * 32 + ln] = (bf16)(b ? s[1][e] : s[0][e]);
+      for (int b = 0; b < 2; ++b) {
+        if (!seen) break;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) mine[(8 * (e >> 2) + 4 * h + (e & 3)) * 32 + ln] = pf[b * 2 + (e >> 3)][e & 7];
         __builtin_amdgcn_wave_barrier();
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
 #pragma unroll 1
@@ -264,7 +299,7 @@ __global__ __launch_bounds__(256, 2) void attend_tiles_kernel(PagedAttnArgs a) {
       }
     if (a.lse && h == 0) a.lse[(size_t)row * a.n_heads + head] = lse_of(m * sl, l);
   } else {
-    float* part = row_part(a, HD, at.n, item * a.c.n_kv_heads + hk, split);
+    float* part = row_part(a, HD, t.n, t.item * a.c.n_kv_heads + hk, t.split);
 #pragma unroll
     for (int c = 0; c < OB; ++c)
 #pragma unroll
@@ -286,12 +321,8 @@ __global__ __launch_bounds__(256, 2) void attend_rows_kernel(PagedAttnArgs a) {
   static_assert(ROW_KEYS<float> == KEY_TILE && ROW_TILE<float> == 64, "four waves of 16 columns");
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, lr = lane & 15, lg = lane >> 4;
   const int hk = blockIdx.x % a.c.n_kv_heads;
-  RowTiles at = row_tiles(a, 0x7fffffff);
-  if (at.n == 0) return;
-  const int split = blockIdx.x / a.c.n_kv_heads / at.n, item = blockIdx.x / a.c.n_kv_heads % at.n;
-  at = row_tiles(a, item);
-  const RowTile<TK> t = row_tile<TK>(a, at);
-  if (split >= t.splits) return;
+  const RowTile<TK> t = row_tile<TK>(a, blockIdx.x / a.c.n_kv_heads);
+  if (t.b < 0) return;
   const int w0 = wave * 16;
   if (w0 >= t.cols) return;
   const int col = t.col0 + min(w0 + lr, t.cols - 1);  // columns past the last one repeat it
@@ -301,11 +332,11 @@ __global__ __launch_bounds__(256, 2) void attend_rows_kernel(PagedAttnArgs a) {
   C c;
   c.clear();
   c.load_q((const float*)a.q + row * a.q_stride + head * HD);
-  const int end = min((split + 1) * t.per, t.keys.n);
-  for (int i = split * t.per; i < end; ++i) {
+  const int end = min((t.split + 1) * t.per, t.keys.n);
+  for (int i = t.split * t.per; i < end; ++i) {
     const int j0 = t.keys.key(i);
     if (none_see(a, lowest, highest, j0, TK)) continue;
-    attend_tile<float, HD, true>(a, hk, j0, page_of<TK>(a.c, at.b, j0), p, lowest, highest, c);
+    attend_tile<float, HD, true>(a, hk, j0, page_of<TK>(a.c, t.b, j0), p, lowest, highest, c);
   }
   const float l = c.sum();
   if (w0 + lr >= t.cols) return;
@@ -318,7 +349,7 @@ __global__ __launch_bounds__(256, 2) void attend_rows_kernel(PagedAttnArgs a) {
       for (int j = 0; j < VJ; ++j) dst[e * VJ + j] = c.o[j][e] * inv;
     if (a.lse && lg == 0) a.lse[(size_t)row * a.n_heads + head] = lse_of(c.m, l);
   } else {
-    float* part = row_part(a, HD, at.n, item * a.c.n_kv_heads + hk, split);
+    float* part = row_part(a, HD, t.n, t.item * a.c.n_kv_heads + hk, t.split);
 #pragma unroll
     for (int e = 0; e < 4; ++e)
 #pragma unroll
