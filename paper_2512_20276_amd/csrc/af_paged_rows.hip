@@ -5,11 +5,6 @@ namespace af {
 
 typedef __attribute__((__vector_size__(4 * sizeof(short)))) short s16x4;
 
-__device__ __forceinline__ const char* uniform(const void* p) {
-  const unsigned lo = __builtin_amdgcn_readfirstlane((unsigned)(uintptr_t)p);
-  const unsigned hi = __builtin_amdgcn_readfirstlane((unsigned)((uintptr_t)p >> 32));
-  return (const char*)((uintptr_t)hi << 32 | lo);
-}
 __device__ __forceinline__ float max_of_halves(float v) {  // of lane % 32 and lane % 32 + 32
   const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
   return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
@@ -24,7 +19,7 @@ struct PageTiles {
   static constexpr int BYTES = KEYS * ROW, STAGE = 2 * BYTES;
   static constexpr int STEP = 64 / CHUNKS;                // rows that a wave's load fills
   static constexpr int LOADS = KEYS / STEP / 4;           // loads of a wave for a tile of keys, and of values
-  static_assert(STEP <= PAGED_MIN_PAGE && KEYS % (STEP * 4) == 0, "a load's rows lie in one page");
+  static_assert(8 % STEP == 0 && PAGED_MIN_PAGE >= 8 && LOADS * STEP == 16, "a load's rows lie in one page");
   __device__ __forceinline__ static int turn(int r) {
     if constexpr (HD == 128) return (r & 3) << 2 | (r >> 2 & 3);
     else return (r >> 1 & 1) << 2 | (r >> 2 & 3);
@@ -77,17 +72,23 @@ __global__ __launch_bounds__(256, 2) void attend_tiles_kernel(PagedAttnArgs a) {
 #pragma unroll
   for (int i = 0; i < L::LOADS; ++i) {
     const int r = (wave * L::LOADS + i) * L::STEP + lane / L::CHUNKS;
-    voff[i] = lane / L::CHUNKS * L::ROW + (lane % L::CHUNKS ^ L::turn(r)) * 16;
+    voff[i] = (i * L::STEP % 8 + lane / L::CHUNKS) * L::ROW + (lane % L::CHUNKS ^ L::turn(r)) * 16;
   }
   const int in_page = (1 << a.c.page_shift) - 1;
   const auto load = [&](int j0, int pages, int buf) {  // pages: of key j0 + lane
+    // a wave's 16 rows, in groups of 8 that lie in one page each
 #pragma unroll
-    for (int i = 0; i < L::LOADS; ++i) {
-      const int r = (wave * L::LOADS + i) * L::STEP;
+    for (int g = 0; g < 2; ++g) {
+      const int r = wave * 16 + g * 8;
       const int page = max(__builtin_amdgcn_readlane(pages, r), 0);
       const size_t at = ((((size_t)page * a.c.n_kv_heads + hk) << a.c.page_shift) + ((j0 + r) & in_page)) * L::ROW;
-      dma16(uniform((const char*)a.c.k + at), voff[i], lds0 + buf * L::STAGE + r * L::ROW);
-      dma16(uniform((const char*)a.c.v + at), voff[i], lds0 + buf * L::STAGE + L::BYTES + r * L::ROW);
+      const unsigned dst = lds0 + buf * L::STAGE + r * L::ROW;
+#pragma unroll
+      for (int i = 0; i < 8 / L::STEP; ++i) {
+        const int n = g * (8 / L::STEP) + i;
+        dma16((const char*)a.c.k + at, voff[n], dst + i * L::STEP * L::ROW);
+        dma16((const char*)a.c.v + at, voff[n], dst + L::BYTES + i * L::STEP * L::ROW);
+      }
     }
   };
 
@@ -122,15 +123,16 @@ __global__ __launch_bounds__(256, 2) void attend_tiles_kernel(PagedAttnArgs a) {
     // this tile is there, and every wave is done with the other one
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
     const unsigned long long there = __ballot(pages >= 0);
+    const int here = pages;
     pages = next_pages;
     if (i + 1 < end) load(t.keys.key(i + 1), pages, buf ^ 1);
     if (i + 2 < end) next_pages = page_of<TK>(a.c, t.b, t.keys.key(i + 2));
     const char* Kt = smem + buf * L::STAGE;
     char* Vt = smem + buf * L::STAGE + L::BYTES;
 
-    // ---- tiles that some column does not see whole: values that nobody sees become zeros, since a probability of 0 does
-    // not hide an infinity or a NaN; where others are not finite, products are taken one by one
-    bool one_by_one = false;
+    // ---- tiles that some column does not see whole: values that nobody sees, or that are not finite, become zeros, since a
+    // probability of 0 does not hide an infinity or a NaN; the columns that see those that are not finite add them below
+    bool odd_values = false;
     if (!(all_see(a, t.lowest, t.highest, j0, TK) && there == ~0ull)) {
       constexpr int T = 256 / TK, N = L::CHUNKS / T;  // threads of a row, chunks of each
       const int r = tid / T;
@@ -139,23 +141,25 @@ __global__ __launch_bounds__(256, 2) void attend_tiles_kernel(PagedAttnArgs a) {
 #pragma unroll
       for (int c = 0; c < N; ++c) {
         uint4* at16 = (uint4*)(Vt + r * L::ROW + (tid % T * N + c) * 16);
-        if (some) {
-          const uint4 w = *at16;
-          const unsigned u[4] = {w.x, w.y, w.z, w.w};
+        const uint4 w = *at16;
+        unsigned u[4] = {w.x, w.y, w.z, w.w};
+        bool here = false;
 #pragma unroll
-          for (int e = 0; e < 4; ++e) odd |= (u[e] & 0x7f80u) == 0x7f80u || (u[e] & 0x7f800000u) == 0x7f800000u;
-        } else {
-          *at16 = zero4();
+        for (int e = 0; e < 4; ++e) {
+          const bool lo = (u[e] & 0x7f80u) == 0x7f80u, hi = (u[e] & 0x7f800000u) == 0x7f800000u;
+          u[e] &= (lo ? 0u : 0xffffu) | (hi ? 0u : 0xffff0000u);
+          here |= lo | hi;
         }
+        if (!some) *at16 = zero4();
+        else if (here) *at16 = make_uint4(u[0], u[1], u[2], u[3]);
+        odd |= some & here;
       }
-      one_by_one = __syncthreads_or(odd);
+      odd_values = __syncthreads_or(odd);
     }
-    const bool seen = busy && !none_see(a, lowest, highest, j0, TK);
-    const bool whole = all_see(a, lowest, highest, j0, TK) && there == ~0ull;
-
+    if (!busy || none_see(a, lowest, highest, j0, TK)) continue;
     f32x16 s[2];
     bf16x8 pf[4];
-    if (seen) {
+    {
       // ---- S^T = K . Q^T, four operands ahead
       bf16x8 kf[2][4];
       const auto read = [&](int g) {  // four of the 2 KST operands
@@ -185,17 +189,32 @@ __global__ __launch_bounds__(256, 2) void attend_tiles_kernel(PagedAttnArgs a) {
           }
         }
       });
-      if (!whole) {
-        // the lane's keys are 4 h on from constants: seen are those up to `last` that lie behind `left` or before `first`
-        const int last = min(p, a.c.cap - 1) - j0 - 4 * h, left = max(p, -1) - a.window - j0 - 4 * h, first = a.sinks - j0 - 4 * h;
-        const unsigned long long mine = there >> (4 * h);
+      // the lane's keys are 4 h on from constants: seen are those up to `last` that lie behind `left` or before `first`
+      if (j0 + TK - 1 > lowest || j0 + TK > a.c.cap) {
+        const int last = min(p, a.c.cap - 1) - j0 - 4 * h;
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+          for (int e = 0; e < 16; ++e)
+            if (b * 32 + 8 * (e >> 2) + (e & 3) > last) s[b][e] = -INFINITY;
+      }
+      if (j0 <= max(highest, -1) - a.window && j0 + TK > a.sinks) {
+        const int left = max(p, -1) - a.window - j0 - 4 * h, first = a.sinks - j0 - 4 * h;
 #pragma unroll
         for (int b = 0; b < 2; ++b)
 #pragma unroll
           for (int e = 0; e < 16; ++e) {
             const int k = b * 32 + 8 * (e >> 2) + (e & 3);
-            if (!(mine >> k & 1) || k > last || (k <= left && k >= first)) s[b][e] = -INFINITY;
+            if ((k <= left) & (k >= first)) s[b][e] = -INFINITY;
           }
+      }
+      if (there != ~0ull) {
+        const unsigned long long mine = there >> (4 * h);
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+          for (int e = 0; e < 16; ++e)
+            if (!(mine >> (b * 32 + 8 * (e >> 2) + (e & 3)) & 1)) s[b][e] = -INFINITY;
       }
       // ---- softmax
       float top = s[0][0];
@@ -224,60 +243,46 @@ __global__ __launch_bounds__(256, 2) void attend_tiles_kernel(PagedAttnArgs a) {
         }
       l += sum[0] + sum[1];
     }
-    if (!one_by_one) {
-      // ---- O^T += V^T . P^T
-      if (seen) {
-        bf16x8 vf[2][OB];
-        const auto read = [&](int k) {
+    // ---- O^T += V^T . P^T
+    bf16x8 vf[2][OB];
+    const auto read = [&](int k) {
 #pragma unroll
-          for (int c = 0; c < OB; ++c) {
-            typedef __attribute__((address_space(3))) s16x4 lds4;
-            const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4*)(Vt + v_at[0][c] + k * 16 * L::ROW));
-            const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4*)(Vt + v_at[1][c] + k * 16 * L::ROW));
-            __builtin_memcpy(&vf[k & 1][c], &lo, 8);
-            __builtin_memcpy((char*)&vf[k & 1][c] + 8, &hi, 8);
-          }
-        };
-        read(0);
-        __builtin_amdgcn_sched_group_barrier(0x100, 2 * OB, 1);
-        static_for<0, 4>([&](auto K) {
-          constexpr int k = decltype(K)::value;
-          if constexpr (k < 3) read(k + 1);
-#pragma unroll
-          for (int c = 0; c < OB; ++c) o[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[k & 1][c], pf[k], o[c], 0, 0, 0);
-          if constexpr (k < 3) {
-#pragma unroll
-            for (int c = 0; c < OB; ++c) {
-              __builtin_amdgcn_sched_group_barrier(0x100, 2, 1);
-              __builtin_amdgcn_sched_group_barrier(0x8, 1, 1);
-            }
-          }
-        });
+      for (int c = 0; c < OB; ++c) {
+        typedef __attribute__((address_space(3))) s16x4 lds4;
+        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4*)(Vt + v_at[0][c] + k * 16 * L::ROW));
+        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4*)(Vt + v_at[1][c] + k * 16 * L::ROW));
+        __builtin_memcpy(&vf[k & 1][c], &lo, 8);
+        __builtin_memcpy((char*)&vf[k & 1][c] + 8, &hi, 8);
       }
-    } else {
-      __syncthreads();  // the keys are done with: a wave's part of them takes its probabilities, 32 keys at a time
-      bf16* mine = (bf16*)(Kt + wave * (L::BYTES / 4));
+    };
+    read(0);
+    __builtin_amdgcn_sched_group_barrier(0x100, 2 * OB, 1);
+    static_for<0, 4>([&](auto K) {
+      constexpr int k = decltype(K)::value;
+      if constexpr (k < 3) read(k + 1);
 #pragma unroll
-      for (int b = 0; b < 2; ++b) {
-        if (!seen) break;
+      for (int c = 0; c < OB; ++c) o[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[k & 1][c], pf[k], o[c], 0, 0, 0);
+      if constexpr (k < 3) {
 #pragma unroll
-        for (int e = 0; e < 16; ++e) mine[(8 * (e >> 2) + 4 * h + (e & 3)) * 32 + ln] = pf[b * 2 + (e >> 3)][e & 7];
-        __builtin_amdgcn_wave_barrier();
-        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-#pragma unroll 1
-        for (int k = 0; k < 32; ++k) {
-          const int r = b * 32 + k;
-          if (!(there >> r & 1) || !sees(a, p, j0 + r)) continue;
-          const float w = (float)mine[k * 32 + ln];
-#pragma unroll
-          for (int c = 0; c < OB; ++c)
-#pragma unroll
-            for (int e = 0; e < 16; ++e) {
-              const int d = 32 * c + 8 * (e >> 2) + 4 * h + (e & 3);
-              o[c][e] += w * (float)*(const bf16*)(Vt + r * L::ROW + ((d / 8) ^ L::turn(r)) * 16 + d % 8 * 2);
-            }
+        for (int c = 0; c < OB; ++c) {
+          __builtin_amdgcn_sched_group_barrier(0x100, 2, 1);
+          __builtin_amdgcn_sched_group_barrier(0x8, 1, 1);
         }
-        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+      }
+    });
+    if (odd_values) {  // a weight above 0 times such a value is that value
+#pragma unroll 1
+      for (int k = 0; k < TK; ++k) {
+        const int page = __builtin_amdgcn_readlane(here, k);
+        if (page < 0 || !sees(a, p, j0 + k)) continue;
+        const bf16* v = (const bf16*)a.c.v + ((((size_t)page * a.c.n_kv_heads + hk) << a.c.page_shift) + ((j0 + k) & in_page)) * HD + 4 * h;
+#pragma unroll
+        for (int c = 0; c < OB; ++c)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) {
+            const bf16 w = v[32 * c + 8 * (e >> 2) + (e & 3)];
+            if (not_finite(w)) o[c][e] += (float)w;
+          }
       }
     }
   }
