@@ -33,20 +33,25 @@ struct AppendArgs {
 };
 hipError_t launch_rope_append(int dtype, int head_dim, const AppendArgs& a, hipStream_t s);
 
+struct Divisor {
+  int d, shift;  // shift < 0: no power of two
+};
+inline Divisor divisor(int d) { return Divisor{d, (d & (d - 1)) == 0 ? __builtin_ctz(d) : -1}; }
+
 struct PagedAttnArgs {
   PagedCache c;
   const void* q;
   void* o;
   float* lse;  // [M][n_heads] or null
   long q_stride, o_stride;
-  int n_heads, group;  // query heads, and those that share a key head
+  int n_heads;
+  Divisor group, n_kv_heads;  // heads that share a key head; key heads
   float scale_log2;    // scale * log2(e)
   int window, sinks;   // window INT_MAX: none
   float* parts;        // partial results of what is split over the keys
   long rows_at;        // floats of them before those of tiles of rows
   int shares;          // requests with a single row: shares of a key head's keys, 0: a workgroup for each request
-  int row_tile;        // other requests: columns of a tile
-  int row_splits;      // and the most parts of a tile's keys
+  int row_splits;      // other requests: the most parts of a tile's keys
 };
 // A partial result: outputs of `cols` columns, then a maximum and a sum for each, in whole chunks of 16 bytes.
 __host__ __device__ inline size_t paged_part_floats(int cols, int hd) { return ((size_t)cols * (hd + 2) + 3) / 4 * 4; }
@@ -60,7 +65,7 @@ constexpr int ROW_GRID = 1024;  // workgroups that a split of tiles of rows is t
 
 // How a call of these sizes is launched, and its workspace.
 struct PagedPlan {
-  int shares, row_tile, row_splits;
+  int shares, row_splits;
   long rows_at, floats;         // floats of workspace before tiles of rows, in all
   int single_grid, row_grid;    // workgroups
   int join_singles, join_rows;  // workgroups of the join, 0: nothing can be split

@@ -120,7 +120,7 @@ __device__ __forceinline__ int share_size(const PagedAttnArgs& a, int total) {
 }
 // Partial results of a share: of a request that began before it, and of one that ends behind it.
 __device__ __forceinline__ float* single_part(const PagedAttnArgs& a, int hd, int share, int head_block, int head_blocks, bool ends_behind) {
-  return a.parts + ((size_t)(share * head_blocks + head_block) * 2 + ends_behind) * paged_part_floats(min(a.group, 16), hd);
+  return a.parts + ((size_t)(share * head_blocks + head_block) * 2 + ends_behind) * paged_part_floats(min(a.group.d, 16), hd);
 }
 
 template <typename T, int HD>
@@ -130,9 +130,9 @@ __global__ __launch_bounds__(256, 2) void attend_single_kernel(PagedAttnArgs a) 
   __shared__ __attribute__((aligned(16))) float wo[SINGLE_WAVES][16][ROW];
   __shared__ float wm[SINGLE_WAVES][16], wl[SINGLE_WAVES][16];
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, lr = lane & 15, lg = lane >> 4;
-  const int blocks = (a.group + 15) / 16, head_blocks = a.c.n_kv_heads * blocks;
+  const int blocks = (a.group.d + 15) / 16, head_blocks = a.c.n_kv_heads * blocks;
   const int hb = blockIdx.x % head_blocks, share = blockIdx.x / head_blocks;
-  const int hk = hb / blocks, col0 = hb % blocks * 16, cols = min(a.group - col0, 16);
+  const int hk = hb / blocks, col0 = hb % blocks * 16, cols = min(a.group.d - col0, 16);
 
   int b = share, at = 0, end = 0x7fffffff, before = 0;
   if (a.shares) {
@@ -157,7 +157,7 @@ __global__ __launch_bounds__(256, 2) void attend_single_kernel(PagedAttnArgs a) 
     const int i0 = at - before, i1 = min(end - before, n), p = r.len - 1;
     C c;
     c.clear();
-    c.load_q(lr < cols ? (const T*)a.q + r.first * a.q_stride + (hk * a.group + col0 + lr) * HD : nullptr);
+    c.load_q(lr < cols ? (const T*)a.q + r.first * a.q_stride + (hk * a.group.d + col0 + lr) * HD : nullptr);
     int i = i0 + wave;
     int page = i < i1 ? page_of<KEY_TILE>(a.c, b, t.key(i)) : -1;
     for (; i < i1; i += SINGLE_WAVES) {
@@ -192,7 +192,7 @@ __global__ __launch_bounds__(256, 2) void attend_single_kernel(PagedAttnArgs a) 
         sum += f * wl[w][col];
         o += f * *(const f32x4*)&wo[w][col][d];
       }
-      const int head = hk * a.group + col0 + col;
+      const int head = hk * a.group.d + col0 + col;
       if (whole) {
         const float inv = sum == 0.f ? 0.f : 1.0f / sum;
         T* dst = (T*)a.o + r.first * a.o_stride + head * HD + d;
@@ -203,8 +203,8 @@ __global__ __launch_bounds__(256, 2) void attend_single_kernel(PagedAttnArgs a) 
         float* part = single_part(a, HD, share, hb, head_blocks, i0 == 0);
         *(f32x4*)(part + col * HD + d) = o;
         if (d == 0) {
-          part[min(a.group, 16) * HD + 2 * col] = m;
-          part[min(a.group, 16) * HD + 2 * col + 1] = sum;
+          part[min(a.group.d, 16) * HD + 2 * col] = m;
+          part[min(a.group.d, 16) * HD + 2 * col + 1] = sum;
         }
       }
     }
@@ -246,8 +246,8 @@ __device__ __forceinline__ void join_single(const PagedAttnArgs& a, int b, int h
   }
   const int per = share_size(a, total), s0 = before / per, n = (before + tiles - 1) / per - s0 + 1;
   if (n == 1) return;
-  const int blocks = (a.group + 15) / 16, head_blocks = a.c.n_kv_heads * blocks, cols = min(a.group, 16);
-  const int hb = head / a.group * blocks + head % a.group / 16, col = head % a.group % 16;
+  const int blocks = (a.group.d + 15) / 16, head_blocks = a.c.n_kv_heads * blocks, cols = min(a.group.d, 16);
+  const int hb = head / a.group.d * blocks + head % a.group.d / 16, col = head % a.group.d % 16;
   const auto part = [&](int i) { return single_part(a, HD, s0 + i, hb, head_blocks, i == 0); };
   const int ml = cols * HD + 2 * col;
   float m = -INFINITY;
@@ -283,25 +283,25 @@ __device__ __forceinline__ void join_single(const PagedAttnArgs& a, int b, int h
 template <typename T, int HD>
 __device__ __forceinline__ void join_rows(const PagedAttnArgs& a, int item, int col_block) {
   constexpr int DT = HD / 16;
-  const RowTile<ROW_KEYS<T>> t = row_tile<ROW_KEYS<T>>(a, item / a.c.n_kv_heads);
+  const RowTile<ROW_KEYS<T>> t = row_tile<ROW_KEYS<T>, ROW_TILE<T>>(a, item / a.c.n_kv_heads);
   if (t.b < 0 || t.split > 0) return;
   const int n = t.splits;
   const int col = col_block * 16 + threadIdx.x / 16, d = threadIdx.x % 16 * DT;
   if (n == 1 || col >= t.cols) return;
   const int hk = item % a.c.n_kv_heads;
   float m = -INFINITY, l = 0.f;
-  for (int i = 0; i < n; ++i) m = fmaxf(m, row_part(a, HD, t.n, item, i)[a.row_tile * HD + 2 * col]);
+  for (int i = 0; i < n; ++i) m = fmaxf(m, row_part(a, ROW_TILE<T>, HD, t.n, item, i)[ROW_TILE<T> * HD + 2 * col]);
   const float ref = m == -INFINITY ? 0.f : m;
   float o[DT] = {};
   for (int i = 0; i < n; ++i) {
-    const float* part = row_part(a, HD, t.n, item, i);
-    const float f = exp2f(part[a.row_tile * HD + 2 * col] - ref);
-    l += f * part[a.row_tile * HD + 2 * col + 1];
+    const float* part = row_part(a, ROW_TILE<T>, HD, t.n, item, i);
+    const float f = exp2f(part[ROW_TILE<T> * HD + 2 * col] - ref);
+    l += f * part[ROW_TILE<T> * HD + 2 * col + 1];
 #pragma unroll
     for (int e = 0; e < DT; ++e) o[e] += f * part[col * HD + d + e];
   }
   const float inv = l == 0.f ? 0.f : 1.0f / l;
-  const int row = t.r.first + (t.col0 + col) / a.group, head = hk * a.group + (t.col0 + col) % a.group;
+  const int row = t.r.first + (t.col0 + col) / a.group.d, head = hk * a.group.d + (t.col0 + col) % a.group.d;
   T* dst = (T*)a.o + row * a.o_stride + head * HD + d;
 #pragma unroll
   for (int e = 0; e < DT; ++e) dst[e] = from_f<T>(o[e] * inv);
@@ -314,7 +314,7 @@ __global__ __launch_bounds__(256) void join_kernel(PagedAttnArgs a, int singles)
   if (i < singles) {
     join_single<T, HD>(a, i / a.n_heads, i % a.n_heads);
   } else {
-    const int blocks = a.row_tile / 16;
+    const int blocks = ROW_TILE<T> / 16;
     join_rows<T, HD>(a, (i - singles) / blocks, (i - singles) % blocks);
   }
 }
@@ -334,18 +334,18 @@ bool paged_plan(int dtype, int head_dim, int n_kv_heads, int n_heads, int n_seq,
     floats = shares * head_blocks * 2 * paged_part_floats(std::min(group, 16), head_dim);
   }
   p->rows_at = floats;
-  p->row_tile = dtype == AF_BF16 ? ROW_TILE<bf16> : ROW_TILE<float>;
   p->row_splits = 1;
+  const int row_tile = dtype == AF_BF16 ? ROW_TILE<bf16> : ROW_TILE<float>;
   if (!single) {
-    const long columns = (long)M * group, tiles = columns / p->row_tile + std::min(n_seq, M / 2);  // at most so many
+    const long columns = (long)M * group, tiles = columns / row_tile + std::min(n_seq, M / 2);  // at most so many
     row_grid = tiles * n_kv_heads;
     const long splits = std::min((long)cap / SPLIT_KEYS + 1, (long)ROW_GRID);
     // requests with a single row take n_seq rows at most; what is left may fill the GPU whatever the lengths are
-    const long sure = (long)std::max(M - n_seq, 0) * group / p->row_tile * n_kv_heads;
+    const long sure = (long)std::max(M - n_seq, 0) * group / row_tile * n_kv_heads;
     if (splits > 1 && sure <= ROW_GRID / 2) {
       p->row_splits = (int)splits;
-      join_rows = tiles * n_kv_heads * (p->row_tile / 16);
-      floats += std::min((long)ROW_GRID, row_grid * splits) * paged_part_floats(p->row_tile, head_dim);
+      join_rows = tiles * n_kv_heads * (row_tile / 16);
+      floats += std::min((long)ROW_GRID, row_grid * splits) * paged_part_floats(row_tile, head_dim);
       row_grid = std::max(row_grid, (long)ROW_GRID);
     }
   }

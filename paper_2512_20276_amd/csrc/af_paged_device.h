@@ -10,6 +10,10 @@ namespace af {
 constexpr int KEY_TILE = 32;
 constexpr int NO_WINDOW = 0x7fffffff;
 
+// Divisors are powers of two as a rule (heads of a group, key heads), and then it is a shift.
+__device__ __forceinline__ int quotient(int x, Divisor d) { return d.shift >= 0 ? x >> d.shift : x / d.d; }
+__device__ __forceinline__ int remainder(int x, Divisor d, int q) { return x - q * d.d; }
+
 struct Request {
   int first, n, len;  // rows [first, first + n), cache length with them
 };
@@ -71,13 +75,20 @@ __device__ __forceinline__ bool none_see(const PagedAttnArgs& a, int lowest, int
   return j0 > highest || j0 >= a.c.cap || (j0 + n - 1 <= max(lowest, -1) - a.window && j0 >= a.sinks);
 }
 
-// The page of key j0 + lane % N, -1 where there is none.
+// The table's entry for key j0 + lane % N, and the page that it means: -1 where there is none.  Apart, so that an entry
+// can be on its way for a while: whatever looks at it waits for all loads before it.
+template <int N>
+__device__ __forceinline__ int page_entry(const PagedCache& c, int b, int j0) {
+  const int at = (j0 + (int)(threadIdx.x & (N - 1))) >> c.page_shift;
+  return c.table[(size_t)b * c.max_pages + min(at, c.max_pages - 1)];
+}
+template <int N>
+__device__ __forceinline__ int page_of_entry(const PagedCache& c, int j0, int entry) {
+  return j0 + (int)(threadIdx.x & (N - 1)) < c.cap && entry >= 0 && entry < c.n_pages ? entry : -1;
+}
 template <int N>
 __device__ __forceinline__ int page_of(const PagedCache& c, int b, int j0) {
-  const int j = j0 + (threadIdx.x & (N - 1));
-  const int at = j >> c.page_shift;
-  const int page = c.table[(size_t)b * c.max_pages + min(at, c.max_pages - 1)];
-  return at < c.max_pages && page >= 0 && page < c.n_pages ? page : -1;
+  return page_of_entry<N>(c, j0, page_entry<N>(c, b, j0));
 }
 
 // Softmax state and output of 16 columns, one for each lane % 16.  Scores are taken transposed, S^T = K . Q^T, and so is
@@ -233,16 +244,16 @@ __device__ __forceinline__ void attend_tile(const PagedAttnArgs& a, int hk, int 
 // The natural logarithm of a column's sum of exponentials from its maximum and sum in powers of two.
 __device__ __forceinline__ float lse_of(float m, float l) { return (m + log2f(l)) * 0.6931471805599453f; }
 
-// Sum and exclusive prefix of an integer over the wave's lanes.
+// Sum and exclusive prefix of an integer over the wave's lanes: within rows of 16 lanes, then over the rows.
 __device__ __forceinline__ int wave_prefix(int v, int& total) {
-  const int lane = threadIdx.x & 63;
   int x = v;
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    const int y = __shfl_up(x, d);
-    if (lane >= d) x += y;
-  }
-  total = __shfl(x, 63);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, true);   // from 1, 2, 4 and 8 lanes below
+  x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, true);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, true);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, true);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);  // lane 15's to the row above, of rows 0 and 2
+  x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);  // lane 31's to the upper half
+  total = __builtin_amdgcn_readlane(x, 63);
   return x - v;
 }
 
@@ -263,7 +274,7 @@ struct RowTile {
 __device__ __forceinline__ int scalar(int v) { return __builtin_amdgcn_readfirstlane(v); }
 // Workgroup `at` of a key head (all parts 0 first).  A request's last tile, whose rows see the most keys, is begun first.
 // The requests are read once by the lanes of a wave, a second time only where they are more than 64.
-template <int TK>
+template <int TK, int COLS>
 __device__ __forceinline__ RowTile<TK> row_tile(const PagedAttnArgs& a, int at) {
   const int lane = threadIdx.x & 63;
   RowTile<TK> t;
@@ -274,17 +285,21 @@ __device__ __forceinline__ RowTile<TK> row_tile(const PagedAttnArgs& a, int at) 
     n = 0;
     if (b0 + lane < a.c.n_seq) {
       r = request_at(a.c, b0 + lane);
-      if (r.n > 1) n = (r.n * a.group + a.row_tile - 1) / a.row_tile;
+      if (r.n > 1) n = (r.n * a.group.d + COLS - 1) / COLS;
     }
     prefix = wave_prefix(n, all);
-    all = scalar(all);
   };
   for (int b0 = 0; b0 < a.c.n_seq; b0 += 64) {
     read(b0);
     t.n += all;
   }
   if (t.n == 0) return t;
-  t.item = at % t.n, t.split = at / t.n;
+  t.item = at, t.split = 0;
+  if (at >= t.n) {
+    if (a.row_splits == 1) return t;
+    t.split = at / t.n;
+    t.item = at - t.split * t.n;
+  }
   for (int b0 = 0, before = 0; b0 < a.c.n_seq; b0 += 64) {
     if (a.c.n_seq > 64) read(b0);
     const unsigned long long past = __ballot(before + prefix + n > t.item);
@@ -292,24 +307,27 @@ __device__ __forceinline__ RowTile<TK> row_tile(const PagedAttnArgs& a, int at) 
       const int l = __builtin_ctzll(past);
       t.b = b0 + l;
       t.r = Request{__builtin_amdgcn_readlane(r.first, l), __builtin_amdgcn_readlane(r.n, l), __builtin_amdgcn_readlane(r.len, l)};
-      t.col0 = (__builtin_amdgcn_readlane(n, l) - 1 - (t.item - before - __builtin_amdgcn_readlane(prefix, l))) * a.row_tile;
+      t.col0 = (__builtin_amdgcn_readlane(n, l) - 1 - (t.item - before - __builtin_amdgcn_readlane(prefix, l))) * COLS;
       break;
     }
     before += all;
   }
-  t.cols = min(a.row_tile, t.r.n * a.group - t.col0);
-  t.lowest = t.r.len - t.r.n + t.col0 / a.group;
-  t.highest = t.r.len - t.r.n + (t.col0 + t.cols - 1) / a.group;
+  t.cols = min(COLS, t.r.n * a.group.d - t.col0);
+  t.lowest = t.r.len - t.r.n + quotient(t.col0, a.group);
+  t.highest = t.r.len - t.r.n + quotient(t.col0 + t.cols - 1, a.group);
   t.keys = key_tiles<TK>(a, t.lowest, t.highest);
-  const int most = min(a.row_splits, max(ROW_GRID / (t.n * a.c.n_kv_heads), 1));
-  t.splits = max(min(most, t.keys.n * TK / SPLIT_KEYS), 1);
-  t.per = (t.keys.n + t.splits - 1) / t.splits;
+  t.splits = 1, t.per = t.keys.n;
+  if (a.row_splits > 1) {
+    const int most = min(a.row_splits, max(ROW_GRID / (t.n * a.c.n_kv_heads), 1));
+    t.splits = max(min(most, t.keys.n * TK / SPLIT_KEYS), 1);
+    t.per = (t.keys.n + t.splits - 1) / t.splits;
+  }
   if (t.split >= t.splits) t.b = -1;
   return t;
 }
-// Partial result of one part: a.row_tile x HD outputs, then a maximum and a sum for each column.
-__device__ __forceinline__ float* row_part(const PagedAttnArgs& a, int hd, int n_tiles, int item, int split) {
-  return a.parts + a.rows_at + ((size_t)split * n_tiles * a.c.n_kv_heads + item) * paged_part_floats(a.row_tile, hd);
+// Partial result of one part: cols x HD outputs, then a maximum and a sum for each column.
+__device__ __forceinline__ float* row_part(const PagedAttnArgs& a, int cols, int hd, int n_tiles, int item, int split) {
+  return a.parts + a.rows_at + ((size_t)split * n_tiles * a.c.n_kv_heads + item) * paged_part_floats(cols, hd);
 }
 
 }  // namespace af

@@ -135,11 +135,11 @@ extern "C" af_status af_op_attention_paged(const af_paged_kv* kv, const void* q,
   }
   if (!aligned(workspace, 16)) return refuse(AF_ERR_INVALID_ARG, me, "the workspace must be 16-byte aligned");
   a.q = q, a.o = o, a.lse = lse, a.q_stride = q_stride, a.o_stride = o_stride;
-  a.n_heads = n_heads, a.group = n_heads / kv->n_kv_heads;
+  a.n_heads = n_heads, a.group = divisor(n_heads / kv->n_kv_heads), a.n_kv_heads = divisor(kv->n_kv_heads);
   a.scale_log2 = (float)(scale * 1.4426950408889634);
   a.window = window ? window : INT_MAX, a.sinks = window ? n_sink : 0;
   a.parts = (float*)workspace, a.rows_at = p.rows_at;
-  a.shares = p.shares, a.row_tile = p.row_tile, a.row_splits = p.row_splits;
+  a.shares = p.shares, a.row_splits = p.row_splits;
   AF_HIP(launch_attention_paged(kv->dtype, kv->head_dim, a, p, (hipStream_t)hip_stream));
   return AF_OK;
 }

@@ -38,20 +38,20 @@ struct PageTiles {
 template <int HD>
 __global__ __launch_bounds__(256, 2) void attend_tiles_kernel(PagedAttnArgs a) {
   typedef PageTiles<HD> L;
-  constexpr int TK = L::KEYS, KST = HD / 16, OB = HD / 32;
+  constexpr int TK = L::KEYS, COLS = ROW_TILE<bf16>, KST = HD / 16, OB = HD / 32;
   __shared__ __attribute__((aligned(1024))) char smem[2 * L::STAGE];
+  __shared__ int odd_tile;  // the last tile, counted from 1, that held such a value as below
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), ln = lane & 31, h = lane >> 5;
-  const int hk = blockIdx.x % a.c.n_kv_heads;
-  const RowTile<TK> t = row_tile<TK>(a, blockIdx.x / a.c.n_kv_heads);
+  const int at = quotient(blockIdx.x, a.n_kv_heads), hk = remainder(blockIdx.x, a.n_kv_heads, at);
+  const RowTile<TK> t = row_tile<TK, COLS>(a, at);
   if (t.b < 0) return;
 
   // ---- the wave's columns (those past the last one repeat it and are not stored)
   const int w0 = wave * 32;
-  const bool busy = w0 < t.cols;
   const int col = t.col0 + min(w0 + ln, t.cols - 1);
-  const int row = t.r.first + col / a.group, head = hk * a.group + col % a.group;
-  const int base = t.r.len - t.r.n, p = base + col / a.group;
-  const int lowest = base + (t.col0 + min(w0, t.cols - 1)) / a.group, highest = base + (t.col0 + min(w0 + 31, t.cols - 1)) / a.group;
+  const int i_row = quotient(col, a.group), row = t.r.first + i_row, head = hk * a.group.d + remainder(col, a.group, i_row);
+  const int base = t.r.len - t.r.n, p = base + i_row;
+  const int lowest = base + quotient(t.col0 + min(w0, t.cols - 1), a.group), highest = base + quotient(t.col0 + min(w0 + 31, t.cols - 1), a.group);
   // a scale below 0 turns the queries' sign, and one of 0 clears them, so that the largest score has the largest product
   const float sign = a.scale_log2 > 0.f ? 1.f : a.scale_log2 < 0.f ? -1.f : 0.f;
   const float sl = a.scale_log2 == 0.f ? 1.f : fabsf(a.scale_log2);
@@ -94,15 +94,14 @@ __global__ __launch_bounds__(256, 2) void attend_tiles_kernel(PagedAttnArgs a) {
 
   // ---- LDS addresses: key ln of a block of 32, chunk 2 s + h; values 4 h + lane % 16 / 4 (and 8 further) of 16, dimensions
   // 16 (lane / 16 % 2) + 4 (lane % 4) of 32
-  const int kz = L::turn(ln) ^ h, x = lane & 15, vr = 4 * h + (x >> 2);
-  const int vc = (lane >> 4 & 1) * 2 + (x >> 1 & 1);
-  const int k_at = ln * L::ROW;
-  int v_at[2][OB];
+  // (a row is as long as its places, so the chunk's bits are turned in the address itself)
+  const int x = lane & 15, vr = 4 * h + (x >> 2), vc = (lane >> 4 & 1) * 2 + (x >> 1 & 1);
+  int k_at = ln * L::ROW + (L::turn(ln) ^ h) * 16;
+  int v_at[2];
 #pragma unroll
-  for (int i = 0; i < 2; ++i)
-#pragma unroll
-    for (int c = 0; c < OB; ++c) v_at[i][c] = (vr + 8 * i) * L::ROW + ((4 * c) ^ (vc ^ L::turn(vr + 8 * i))) * 16 + (x & 1) * 8;
+  for (int i = 0; i < 2; ++i) v_at[i] = L::BYTES + (vr + 8 * i) * L::ROW + (vc ^ L::turn(vr + 8 * i)) * 16 + (x & 1) * 8;
 
+  if (tid == 0) odd_tile = 0;
   f32x16 o[OB];
 #pragma unroll
   for (int c = 0; c < OB; ++c)
@@ -110,30 +109,25 @@ __global__ __launch_bounds__(256, 2) void attend_tiles_kernel(PagedAttnArgs a) {
     for (int e = 0; e < 16; ++e) o[c][e] = 0.f;
   float m = -INFINITY, l = 0.f;
 
-  int i = t.split * t.per;
-  const int end = min(i + t.per, t.keys.n);
-  int pages = -1, next_pages = -1;
-  if (i < end) {
-    pages = page_of<TK>(a.c, t.b, t.keys.key(i));
-    load(t.keys.key(i), pages, 0);
-    if (i + 1 < end) next_pages = page_of<TK>(a.c, t.b, t.keys.key(i + 1));
+  // ---- the tiles: in LDS by turns, tile i + 1 on its way while tile i is worked on
+  const int i0 = t.split * t.per, end = min(i0 + t.per, t.keys.n);
+  // tiles of keys in [full_from, full_end), or before full_sinks, are seen whole by all columns
+  const int full_end = min(t.lowest, a.c.cap - 1) + 1, full_from = max(t.highest, -1) - a.window + 1;
+  int pages = -1, entry = -1;  // of this tile's keys; of the next one's, as the table has it
+  int next = t.keys.key(i0);
+  if (i0 < end) {
+    pages = page_of<TK>(a.c, t.b, next);
+    load(next, pages, 0);
+    if (i0 + 1 < end) entry = page_entry<TK>(a.c, t.b, t.keys.key(i0 + 1));
   }
-  for (int buf = 0; i < end; ++i, buf ^= 1) {
-    const int j0 = t.keys.key(i);
-    // this tile is there, and every wave is done with the other one
-    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-    const unsigned long long there = __ballot(pages >= 0);
-    const int here = pages;
-    pages = next_pages;
-    if (i + 1 < end) load(t.keys.key(i + 1), pages, buf ^ 1);
-    if (i + 2 < end) next_pages = page_of<TK>(a.c, t.b, t.keys.key(i + 2));
-    const char* Kt = smem + buf * L::STAGE;
-    char* Vt = smem + buf * L::STAGE + L::BYTES;
-
+  // Edge: some column does not see the whole tile
+  const auto work = [&](auto Edge, int i, int j0, unsigned long long there, int here, int buf) {
+    constexpr bool edge = decltype(Edge)::value;
     // ---- tiles that some column does not see whole: values that nobody sees, or that are not finite, become zeros, since a
     // probability of 0 does not hide an infinity or a NaN; the columns that see those that are not finite add them below
     bool odd_values = false;
-    if (!(all_see(a, t.lowest, t.highest, j0, TK) && there == ~0ull)) {
+    if constexpr (edge) {
+      char* const Vt = smem + buf * L::STAGE + L::BYTES;
       constexpr int T = 256 / TK, N = L::CHUNKS / T;  // threads of a row, chunks of each
       const int r = tid / T;
       const bool some = (there >> r & 1) && some_see(a, t.lowest, t.highest, j0 + r);
@@ -154,9 +148,22 @@ __global__ __launch_bounds__(256, 2) void attend_tiles_kernel(PagedAttnArgs a) {
         else if (here) *at16 = make_uint4(u[0], u[1], u[2], u[3]);
         odd |= some & here;
       }
-      odd_values = __syncthreads_or(odd);
+      if (odd) odd_tile = i + 1;
+      __syncthreads();
+      odd_values = odd_tile == i + 1;
+      if (none_see(a, lowest, highest, j0, TK)) return;
     }
-    if (!busy || none_see(a, lowest, highest, j0, TK)) continue;
+    bf16x8 vf[2][OB];
+    const auto read_v = [&](int k) {
+#pragma unroll
+      for (int c = 0; c < OB; ++c) {
+        typedef __attribute__((address_space(3))) s16x4 lds4;
+        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4*)(smem + (v_at[0] ^ c * 64) + k * 16 * L::ROW));
+        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4*)(smem + (v_at[1] ^ c * 64) + k * 16 * L::ROW));
+        __builtin_memcpy(&vf[k & 1][c], &lo, 8);
+        __builtin_memcpy((char*)&vf[k & 1][c] + 8, &hi, 8);
+      }
+    };
     f32x16 s[2];
     bf16x8 pf[4];
     {
@@ -165,7 +172,7 @@ __global__ __launch_bounds__(256, 2) void attend_tiles_kernel(PagedAttnArgs a) {
       const auto read = [&](int g) {  // four of the 2 KST operands
 #pragma unroll
         for (int c = 0; c < 4; ++c)
-          kf[g & 1][c] = *(const bf16x8*)(Kt + k_at + (4 * g + c) / KST * 32 * L::ROW + ((2 * ((4 * g + c) % KST)) ^ kz) * 16);
+          kf[g & 1][c] = *(const bf16x8*)(smem + (k_at ^ (4 * g + c) % KST * 32) + (4 * g + c) / KST * 32 * L::ROW);
       };
 #pragma unroll
       for (int b = 0; b < 2; ++b)
@@ -189,33 +196,36 @@ __global__ __launch_bounds__(256, 2) void attend_tiles_kernel(PagedAttnArgs a) {
           }
         }
       });
-      // the lane's keys are 4 h on from constants: seen are those up to `last` that lie behind `left` or before `first`
-      if (j0 + TK - 1 > lowest || j0 + TK > a.c.cap) {
-        const int last = min(p, a.c.cap - 1) - j0 - 4 * h;
+      if constexpr (edge) {
+        // the lane's keys are 4 h on from constants: seen are those up to `last` that lie behind `left` or before `first`
+        if (j0 + TK - 1 > lowest || j0 + TK > a.c.cap) {
+          const int last = min(p, a.c.cap - 1) - j0 - 4 * h;
 #pragma unroll
-        for (int b = 0; b < 2; ++b)
+          for (int b = 0; b < 2; ++b)
 #pragma unroll
-          for (int e = 0; e < 16; ++e)
-            if (b * 32 + 8 * (e >> 2) + (e & 3) > last) s[b][e] = -INFINITY;
+            for (int e = 0; e < 16; ++e)
+              if (b * 32 + 8 * (e >> 2) + (e & 3) > last) s[b][e] = -INFINITY;
+        }
+        if (j0 <= max(highest, -1) - a.window && j0 + TK > a.sinks) {
+          const int left = max(p, -1) - a.window - j0 - 4 * h, first = a.sinks - j0 - 4 * h;
+#pragma unroll
+          for (int b = 0; b < 2; ++b)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+              const int k = b * 32 + 8 * (e >> 2) + (e & 3);
+              if ((k <= left) & (k >= first)) s[b][e] = -INFINITY;
+            }
+        }
+        if (there != ~0ull) {
+          const unsigned long long mine = there >> (4 * h);
+#pragma unroll
+          for (int b = 0; b < 2; ++b)
+#pragma unroll
+            for (int e = 0; e < 16; ++e)
+              if (!(mine >> (b * 32 + 8 * (e >> 2) + (e & 3)) & 1)) s[b][e] = -INFINITY;
+        }
       }
-      if (j0 <= max(highest, -1) - a.window && j0 + TK > a.sinks) {
-        const int left = max(p, -1) - a.window - j0 - 4 * h, first = a.sinks - j0 - 4 * h;
-#pragma unroll
-        for (int b = 0; b < 2; ++b)
-#pragma unroll
-          for (int e = 0; e < 16; ++e) {
-            const int k = b * 32 + 8 * (e >> 2) + (e & 3);
-            if ((k <= left) & (k >= first)) s[b][e] = -INFINITY;
-          }
-      }
-      if (there != ~0ull) {
-        const unsigned long long mine = there >> (4 * h);
-#pragma unroll
-        for (int b = 0; b < 2; ++b)
-#pragma unroll
-          for (int e = 0; e < 16; ++e)
-            if (!(mine >> (b * 32 + 8 * (e >> 2) + (e & 3)) & 1)) s[b][e] = -INFINITY;
-      }
+      read_v(0);  // in time for the products
       // ---- softmax
       float top = s[0][0];
 #pragma unroll
@@ -244,22 +254,9 @@ __global__ __launch_bounds__(256, 2) void attend_tiles_kernel(PagedAttnArgs a) {
       l += sum[0] + sum[1];
     }
     // ---- O^T += V^T . P^T
-    bf16x8 vf[2][OB];
-    const auto read = [&](int k) {
-#pragma unroll
-      for (int c = 0; c < OB; ++c) {
-        typedef __attribute__((address_space(3))) s16x4 lds4;
-        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4*)(Vt + v_at[0][c] + k * 16 * L::ROW));
-        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4*)(Vt + v_at[1][c] + k * 16 * L::ROW));
-        __builtin_memcpy(&vf[k & 1][c], &lo, 8);
-        __builtin_memcpy((char*)&vf[k & 1][c] + 8, &hi, 8);
-      }
-    };
-    read(0);
-    __builtin_amdgcn_sched_group_barrier(0x100, 2 * OB, 1);
     static_for<0, 4>([&](auto K) {
       constexpr int k = decltype(K)::value;
-      if constexpr (k < 3) read(k + 1);
+      if constexpr (k < 3) read_v(k + 1);
 #pragma unroll
       for (int c = 0; c < OB; ++c) o[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[k & 1][c], pf[k], o[c], 0, 0, 0);
       if constexpr (k < 3) {
@@ -270,7 +267,7 @@ __global__ __launch_bounds__(256, 2) void attend_tiles_kernel(PagedAttnArgs a) {
         }
       }
     });
-    if (odd_values) {  // a weight above 0 times such a value is that value
+    if (edge && odd_values) {  // a weight above 0 times such a value is that value
 #pragma unroll 1
       for (int k = 0; k < TK; ++k) {
         const int page = __builtin_amdgcn_readlane(here, k);
@@ -285,34 +282,77 @@ __global__ __launch_bounds__(256, 2) void attend_tiles_kernel(PagedAttnArgs a) {
           }
       }
     }
+  };
+  // Takes turns: waits for tile i and sends for tile i + 1; whether all columns see tile i whole.
+  int i = i0, buf = 0, j0 = 0, here = -1;
+  unsigned long long there = 0;
+  const auto turn = [&]() {
+    j0 = next;
+    // this tile is there, and every wave is done with the other one
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    there = __ballot(pages >= 0);
+    here = pages;
+    if (i + 1 < end) {
+      next = t.keys.key(i + 1);
+      pages = page_of_entry<TK>(a.c, next, entry);
+      load(next, pages, buf ^ 1);
+      if (i + 2 < end) entry = page_entry<TK>(a.c, t.b, t.keys.key(i + 2));
+    }
+    return j0 + TK <= full_end && (j0 >= full_from || j0 + TK <= a.sinks) && there == ~0ull;
+  };
+  const auto done = [&]() {
+    k_at ^= L::STAGE, v_at[0] ^= L::STAGE, v_at[1] ^= L::STAGE;
+    buf ^= 1;
+    ++i;
+  };
+  while (i < end) {
+    bool whole = turn();
+    if (whole) {
+      do {
+        work(std::false_type{}, i, j0, there, here, buf);
+        done();
+        if (i >= end) break;
+        whole = turn();
+      } while (whole);
+      if (i >= end) break;
+    }
+    work(std::true_type{}, i, j0, there, here, buf);
+    done();
   }
 
-  if (!busy) return;
   l += __shfl_xor(l, 32);
-  if (w0 + ln >= t.cols) return;
+  const bool real = w0 + ln < t.cols;
   if (t.splits == 1) {
     const float inv = l == 0.f ? 0.f : 1.0f / l;
-    bf16* dst = (bf16*)a.o + row * a.o_stride + head * HD + 4 * h;
+    // a lane has four of every eight dimensions, its other half the others: halves are exchanged so that each has eight in a row
+    bf16* dst = (bf16*)a.o + row * a.o_stride + head * HD + 8 * h;
 #pragma unroll
     for (int c = 0; c < OB; ++c)
 #pragma unroll
-      for (int b = 0; b < 4; ++b) {
-        bf16x4 w;
+      for (int b = 0; b < 4; b += 2) {
+        uint2 w[2];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) w[e] = (bf16)(o[c][4 * b + e] * inv);
-        *(bf16x4*)(dst + 32 * c + 8 * b) = w;
+        for (int i = 0; i < 2; ++i) {
+          bf16x4 v;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) v[e] = (bf16)(o[c][4 * (b + i) + e] * inv);
+          __builtin_memcpy(&w[i], &v, 8);
+        }
+        const auto x0 = __builtin_amdgcn_permlane32_swap(w[0].x, w[1].x, false, false);
+        const auto x1 = __builtin_amdgcn_permlane32_swap(w[0].y, w[1].y, false, false);
+        if (real) *(uint4*)(dst + 32 * c + 8 * b) = make_uint4(x0[0], x1[0], x0[1], x1[1]);
       }
-    if (a.lse && h == 0) a.lse[(size_t)row * a.n_heads + head] = lse_of(m * sl, l);
-  } else {
-    float* part = row_part(a, HD, t.n, t.item * a.c.n_kv_heads + hk, t.split);
+    if (a.lse && h == 0 && real) a.lse[(size_t)row * a.n_heads + head] = lse_of(m * sl, l);
+  } else if (real) {
+    float* part = row_part(a, COLS, HD, t.n, t.item * a.c.n_kv_heads + hk, t.split);
 #pragma unroll
     for (int c = 0; c < OB; ++c)
 #pragma unroll
       for (int b = 0; b < 4; ++b)
         *(f32x4*)(part + (w0 + ln) * HD + 32 * c + 8 * b + 4 * h) = f32x4{o[c][4 * b], o[c][4 * b + 1], o[c][4 * b + 2], o[c][4 * b + 3]};
     if (h == 0) {
-      part[a.row_tile * HD + 2 * (w0 + ln)] = m * sl;
-      part[a.row_tile * HD + 2 * (w0 + ln) + 1] = l;
+      part[COLS * HD + 2 * (w0 + ln)] = m * sl;
+      part[COLS * HD + 2 * (w0 + ln) + 1] = l;
     }
   }
 }
@@ -322,18 +362,18 @@ __global__ __launch_bounds__(256, 2) void attend_tiles_kernel(PagedAttnArgs a) {
 template <int HD>
 __global__ __launch_bounds__(256, 2) void attend_rows_kernel(PagedAttnArgs a) {
   typedef Columns<float, HD> C;
-  constexpr int VJ = C::VJ, TK = KEY_TILE;
+  constexpr int VJ = C::VJ, TK = KEY_TILE, COLS = ROW_TILE<float>;
   static_assert(ROW_KEYS<float> == KEY_TILE && ROW_TILE<float> == 64, "four waves of 16 columns");
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, lr = lane & 15, lg = lane >> 4;
-  const int hk = blockIdx.x % a.c.n_kv_heads;
-  const RowTile<TK> t = row_tile<TK>(a, blockIdx.x / a.c.n_kv_heads);
+  const int at = quotient(blockIdx.x, a.n_kv_heads), hk = remainder(blockIdx.x, a.n_kv_heads, at);
+  const RowTile<TK> t = row_tile<TK, COLS>(a, at);
   if (t.b < 0) return;
   const int w0 = wave * 16;
   if (w0 >= t.cols) return;
   const int col = t.col0 + min(w0 + lr, t.cols - 1);  // columns past the last one repeat it
-  const int row = t.r.first + col / a.group, head = hk * a.group + col % a.group;
-  const int base = t.r.len - t.r.n, p = base + col / a.group;
-  const int lowest = base + (t.col0 + w0) / a.group, highest = base + (t.col0 + min(w0 + 15, t.cols - 1)) / a.group;
+  const int i_row = quotient(col, a.group), row = t.r.first + i_row, head = hk * a.group.d + remainder(col, a.group, i_row);
+  const int base = t.r.len - t.r.n, p = base + i_row;
+  const int lowest = base + quotient(t.col0 + w0, a.group), highest = base + quotient(t.col0 + min(w0 + 15, t.cols - 1), a.group);
   C c;
   c.clear();
   c.load_q((const float*)a.q + row * a.q_stride + head * HD);
@@ -354,14 +394,14 @@ __global__ __launch_bounds__(256, 2) void attend_rows_kernel(PagedAttnArgs a) {
       for (int j = 0; j < VJ; ++j) dst[e * VJ + j] = c.o[j][e] * inv;
     if (a.lse && lg == 0) a.lse[(size_t)row * a.n_heads + head] = lse_of(c.m, l);
   } else {
-    float* part = row_part(a, HD, t.n, t.item * a.c.n_kv_heads + hk, t.split);
+    float* part = row_part(a, COLS, HD, t.n, t.item * a.c.n_kv_heads + hk, t.split);
 #pragma unroll
     for (int e = 0; e < 4; ++e)
 #pragma unroll
       for (int j = 0; j < VJ; ++j) part[(w0 + lr) * HD + (lg * 4 + e) * VJ + j] = c.o[j][e];
     if (lg == 0) {
-      part[a.row_tile * HD + 2 * (w0 + lr)] = c.m;
-      part[a.row_tile * HD + 2 * (w0 + lr) + 1] = l;
+      part[COLS * HD + 2 * (w0 + lr)] = c.m;
+      part[COLS * HD + 2 * (w0 + lr) + 1] = l;
     }
   }
 }
