@@ -48,10 +48,11 @@ struct PagedAttnArgs {
   Divisor group, n_kv_heads;  // heads that share a key head; key heads
   float scale_log2;    // scale * log2(e)
   int window, sinks;   // window INT_MAX: none
-  float* parts;        // partial results of what is split over the keys
-  long rows_at;        // floats of them before those of tiles of rows
+  float* parts;        // what is left for the join, and partial results of what is split over the keys
+  long parts_at, rows_at;  // floats before those of shares (the join's words), and before those of tiles of rows
   int shares;          // requests with a single row: shares of a key head's keys, 0: a workgroup for each request
-  int row_splits;      // other requests: the most parts of a tile's keys
+  int single_waves;    // and its waves for each, 1, 2 or 4
+  int row_split;       // other requests: a tile's keys may be split
 };
 // A partial result: outputs of `cols` columns, then a maximum and a sum for each, in whole chunks of 16 bytes.
 __host__ __device__ inline size_t paged_part_floats(int cols, int hd) { return ((size_t)cols * (hd + 2) + 3) / 4 * 4; }
@@ -60,19 +61,20 @@ template <typename T>
 constexpr int ROW_TILE = sizeof(T) == 2 ? 128 : 64;
 template <typename T>
 constexpr int ROW_KEYS = sizeof(T) == 2 ? 64 : 32;
-constexpr int SPLIT_KEYS = 512;
-constexpr int ROW_GRID = 1024;  // workgroups that a split of tiles of rows is to give
+constexpr int SPLIT_TILES = 16;
+constexpr int ROW_GRID = 512;  // workgroups that a split of tiles of rows is to give
 
 // How a call of these sizes is launched, and its workspace.
 struct PagedPlan {
-  int shares, row_splits;
-  long rows_at, floats;         // floats of workspace before tiles of rows, in all
-  int single_grid, row_grid;    // workgroups
+  int shares, single_waves, row_split;
+  long parts_at, rows_at, floats;  // floats of workspace before shares, before tiles of rows, in all
+  int single_grid, row_grid;       // workgroups of single rows, of tiles of rows
+  int tile_grid;                   // of these, as many as there can be tiles
   int join_singles, join_rows;  // workgroups of the join, 0: nothing can be split
 };
 // False: more workgroups than a launch takes.
 bool paged_plan(int dtype, int head_dim, int n_kv_heads, int n_heads, int n_seq, bool single, int M, int cap, PagedPlan* p);
 hipError_t launch_attention_paged(int dtype, int head_dim, const PagedAttnArgs& a, const PagedPlan& p, hipStream_t s);
-hipError_t launch_paged_rows(int dtype, int head_dim, const PagedAttnArgs& a, int grid, hipStream_t s);
+hipError_t launch_paged_rows(int dtype, int head_dim, const PagedAttnArgs& a, const PagedPlan& p, hipStream_t s);
 
 }  // namespace af

@@ -10,6 +10,7 @@ namespace af {
 constexpr int KEY_TILE = 32;
 constexpr int NO_WINDOW = 0x7fffffff;
 
+__device__ __forceinline__ int scalar(int v) { return __builtin_amdgcn_readfirstlane(v); }
 // Divisors are powers of two as a rule (heads of a group, key heads), and then it is a shift.
 __device__ __forceinline__ int quotient(int x, Divisor d) { return d.shift >= 0 ? x >> d.shift : x / d.d; }
 __device__ __forceinline__ int remainder(int x, Divisor d, int q) { return x - q * d.d; }
@@ -264,70 +265,234 @@ __device__ __forceinline__ int wave_prefix(int v, int& total) {
 template <int TK>
 struct RowTile {
   int b;                // the request, -1: nothing to do
-  int n, item, split;   // tiles of all requests, the one that is taken, the part of its keys
   Request r;
   int col0, cols;       // columns [col0, col0 + cols) of the request
   int lowest, highest;  // positions of the first and the last
   KeyTiles<TK> keys;
-  int splits, per;      // parts that the key tiles are cut into, tiles of a part
+  int split, splits;    // the part of the tile's keys, of so many
+  int from, end;        // its key tiles
+  int part0;            // partial results of all tiles before this one's
 };
-__device__ __forceinline__ int scalar(int v) { return __builtin_amdgcn_readfirstlane(v); }
-// Workgroup `at` of a key head (all parts 0 first).  A request's last tile, whose rows see the most keys, is begun first.
+// Where few rows meet many keys the keys are cut into parts of a length that gives about ROW_GRID workgroups (of
+// SPLIT_TILES key tiles at least), about the same for all requests.  Every tile of a request is given as many parts as its
+// last one, whose rows see the most keys, takes; tiles that take fewer leave the others idle, and the last part takes
+// what is left.  A request's last tile is begun first.  Workgroup `at` of a key head: its tile and part; JOIN: tile `at`, part 0.
 // The requests are read once by the lanes of a wave, a second time only where they are more than 64.
-template <int TK, int COLS>
+template <int TK, int COLS, bool JOIN = false>
 __device__ __forceinline__ RowTile<TK> row_tile(const PagedAttnArgs& a, int at) {
   const int lane = threadIdx.x & 63;
   RowTile<TK> t;
-  t.b = -1, t.n = 0;
+  t.b = -1;
   Request r{0, 0, 0};
-  int n = 0, prefix = 0, all = 0;
+  int n = 0, most = 0;  // tiles of the lane's request, key tiles of its last one
   const auto read = [&](int b0) {
     n = 0;
     if (b0 + lane < a.c.n_seq) {
       r = request_at(a.c, b0 + lane);
       if (r.n > 1) n = (r.n * a.group.d + COLS - 1) / COLS;
     }
-    prefix = wave_prefix(n, all);
+    if (a.row_split) most = key_tiles<TK>(a, r.len - min(r.n, quotient(COLS - 1, a.group) + 1), r.len - 1).n;
   };
+  int per = 1 << 30;  // key tiles of a part
+  if (!a.row_split && a.c.n_seq <= 64) {
+    read(0);
+  } else {
+    float work = 0.f;
+    for (int b0 = 0; b0 < a.c.n_seq; b0 += 64) {
+      read(b0);
+      float w = (float)n * (float)most;
+#pragma unroll
+      for (int d = 1; d < 64; d <<= 1) w += __shfl_xor(w, d);
+      work += w;
+    }
+    // (more than any tile has if work is past what fits)
+    if (a.row_split) per = scalar(max((int)fminf(work * a.c.n_kv_heads * (1.0f / ROW_GRID), 1e9f) + 1, SPLIT_TILES));
+  }
+  int before = 0, parts_before = 0, each = 1;
   for (int b0 = 0; b0 < a.c.n_seq; b0 += 64) {
-    read(b0);
-    t.n += all;
-  }
-  if (t.n == 0) return t;
-  t.item = at, t.split = 0;
-  if (at >= t.n) {
-    if (a.row_splits == 1) return t;
-    t.split = at / t.n;
-    t.item = at - t.split * t.n;
-  }
-  for (int b0 = 0, before = 0; b0 < a.c.n_seq; b0 += 64) {
     if (a.c.n_seq > 64) read(b0);
-    const unsigned long long past = __ballot(before + prefix + n > t.item);
+    const int parts = a.row_split ? max((most + per - 1) / per, 1) : 1;
+    int all, all_parts = 0;
+    const int prefix = wave_prefix(JOIN ? n : n * parts, all), of_parts = JOIN ? wave_prefix(n * parts, all_parts) : 0;
+    const unsigned long long past = __ballot(before + prefix + (JOIN ? n : n * parts) > at);
     if (past) {
       const int l = __builtin_ctzll(past);
       t.b = b0 + l;
       t.r = Request{__builtin_amdgcn_readlane(r.first, l), __builtin_amdgcn_readlane(r.n, l), __builtin_amdgcn_readlane(r.len, l)};
-      t.col0 = (__builtin_amdgcn_readlane(n, l) - 1 - (t.item - before - __builtin_amdgcn_readlane(prefix, l))) * COLS;
+      each = __builtin_amdgcn_readlane(parts, l);
+      if (each > 1) per = (__builtin_amdgcn_readlane(most, l) + each - 1) / each;
+      const int within = at - before - __builtin_amdgcn_readlane(prefix, l);
+      const int tile = JOIN || each == 1 ? within : within / each;
+      t.split = JOIN ? 0 : within - tile * each;
+      t.part0 = JOIN ? parts_before + __builtin_amdgcn_readlane(of_parts, l) + within * each : at - t.split;
+      t.col0 = (__builtin_amdgcn_readlane(n, l) - 1 - tile) * COLS;
       break;
     }
     before += all;
+    parts_before += all_parts;
   }
+  if (t.b < 0) return t;
   t.cols = min(COLS, t.r.n * a.group.d - t.col0);
   t.lowest = t.r.len - t.r.n + quotient(t.col0, a.group);
   t.highest = t.r.len - t.r.n + quotient(t.col0 + t.cols - 1, a.group);
   t.keys = key_tiles<TK>(a, t.lowest, t.highest);
-  t.splits = 1, t.per = t.keys.n;
-  if (a.row_splits > 1) {
-    const int most = min(a.row_splits, max(ROW_GRID / (t.n * a.c.n_kv_heads), 1));
-    t.splits = max(min(most, t.keys.n * TK / SPLIT_KEYS), 1);
-    t.per = (t.keys.n + t.splits - 1) / t.splits;
-  }
+  t.splits = each == 1 ? 1 : max(min((t.keys.n + per - 1) / per, each), 1);
+  t.from = t.split * per;
+  t.end = t.split == t.splits - 1 ? t.keys.n : t.from + per;
   if (t.split >= t.splits) t.b = -1;
   return t;
 }
 // Partial result of one part: cols x HD outputs, then a maximum and a sum for each column.
-__device__ __forceinline__ float* row_part(const PagedAttnArgs& a, int cols, int hd, int n_tiles, int item, int split) {
-  return a.parts + a.rows_at + ((size_t)split * n_tiles * a.c.n_kv_heads + item) * paged_part_floats(cols, hd);
+__device__ __forceinline__ float* row_part(const PagedAttnArgs& a, int cols, int hd, int part, int hk) {
+  return a.parts + a.rows_at + ((size_t)part * a.c.n_kv_heads + hk) * paged_part_floats(cols, hd);
+}
+
+// ------------------------------------------------------------------ requests with a single row
+// The heads that share a key head are the columns of a workgroup (16 at most; more take several), whose
+// waves take the tiles of 32 keys in turn and merge in LDS.
+//
+// Which keys a workgroup takes is found on the device, from the lengths as they are when the kernel runs: the key
+// tiles of all requests, one behind the other, are cut into a.shares equal shares (of SHARE_TILES tiles at least), and every
+// key head has a workgroup for each.  A share may end within a request and hold several.  A request counts
+// PIECE_TILES more than it has, before its first one, for what it costs a workgroup to begin and to end one.  What
+// does not hold all of a request's tiles is left as a partial result (output, maximum, sum) for the join, and the
+// workgroup of its first tile leaves the join word of which shares hold it.
+// Short caches are not split (a.shares 0): a.single_waves of a workgroup's four waves take a request's key head.
+constexpr int SINGLE_WAVES = 4;
+constexpr int SHARE_TILES = 4;
+constexpr int PIECE_TILES = 2;
+
+__device__ __forceinline__ int single_tiles(const PagedAttnArgs& a, const Request& r, KeyTiles<KEY_TILE>& t) {
+  t = key_tiles<KEY_TILE>(a, r.len - 1, r.len - 1);
+  return r.n == 1 ? t.n : 0;
+}
+// Partial results of a share: of a request that began before it, and of one that ends behind it.
+__device__ __forceinline__ float* single_part(const PagedAttnArgs& a, int hd, int share, int head_block, int head_blocks, bool ends_behind) {
+  return a.parts + a.parts_at + ((size_t)(share * head_blocks + head_block) * 2 + ends_behind) * paged_part_floats(min(a.group.d, 16), hd);
+}
+
+template <int HD>
+struct SingleLds {
+  static constexpr int ROW = HD + 4;  // padded: columns on different banks
+  float o[SINGLE_WAVES][16][ROW], m[SINGLE_WAVES][16], l[SINGLE_WAVES][16];
+};
+
+template <typename T, int HD>
+__device__ __forceinline__ void attend_single(const PagedAttnArgs& a, int block, SingleLds<HD>& lds) {
+  typedef Columns<T, HD> C;
+  constexpr int VJ = C::VJ;
+  const int tid = threadIdx.x, wave = scalar(tid >> 6), lane = tid & 63, lr = lane & 15, lg = lane >> 4;
+  const int waves = a.shares ? SINGLE_WAVES : a.single_waves, sub = wave / waves;  // of a request; which of the workgroup's
+  const int blocks = (a.group.d + 15) / 16, head_blocks = a.c.n_kv_heads * blocks;
+  const int item = block * (SINGLE_WAVES / waves) + sub, share = item / head_blocks, hb = item % head_blocks;
+  const int hk = hb / blocks, col0 = hb % blocks * 16, cols = min(a.group.d - col0, 16);
+
+  int b = share, at = 0, end = 0x7fffffff, before = 0, per = 0x7fffffff;
+  if (a.shares) {
+    Request r{0, 0, 0};
+    KeyTiles<KEY_TILE> t;
+    int n = 0, prefix = 0, all = 0, total = 0;
+    const auto read = [&](int b0) {
+      n = 0;
+      if (b0 + lane < a.c.n_seq) {
+        r = request_at(a.c, b0 + lane);
+        n = single_tiles(a, r, t);
+        if (n) n += PIECE_TILES;
+      }
+      prefix = wave_prefix(n, all);
+    };
+    for (int b0 = 0; b0 < a.c.n_seq; b0 += 64) {
+      read(b0);
+      total += all;
+    }
+    per = max((total + a.shares - 1) / a.shares, SHARE_TILES);
+    at = share * per;
+    end = min(at + per, total);
+    if (at >= end) return;
+    for (int b0 = 0;; b0 += 64) {
+      if (a.c.n_seq > 64) read(b0);
+      const unsigned long long past = __ballot(before + prefix + n > at);
+      if (past) {
+        const int l = __builtin_ctzll(past);
+        b = b0 + l;
+        before += __builtin_amdgcn_readlane(prefix, l);
+        break;
+      }
+      before += all;
+    }
+  }
+  for (;;) {
+    const bool there = b < a.c.n_seq;  // (not so: a wave without a request, beside ones with one)
+    const Request r = request_at(a.c, there ? b : 0);
+    KeyTiles<KEY_TILE> t;
+    const int n = there ? single_tiles(a, r, t) : 0;
+    const int lead = a.shares && n ? PIECE_TILES : 0;
+    const int i0 = max(at - before - lead, 0), i1 = min(end - before - lead, n), p = r.len - 1;
+    const bool whole = i0 == 0 && i1 == n;
+    C c;
+    c.clear();
+    if (i0 < i1 || !a.shares) {
+      if (i0 < i1) c.load_q(lr < cols ? (const T*)a.q + r.first * a.q_stride + (hk * a.group.d + col0 + lr) * HD : nullptr);
+      int i = i0 + wave % waves;
+      int entry = i < i1 ? page_entry<KEY_TILE>(a.c, b, t.key(i)) : -1;
+      for (; i < i1; i += waves) {
+        const int page = page_of_entry<KEY_TILE>(a.c, t.key(i), entry);
+        if (i + waves < i1) entry = page_entry<KEY_TILE>(a.c, b, t.key(i + waves));
+        attend_tile<T, HD, false>(a, hk, t.key(i), page, p, p, p, c);
+      }
+      // ---- the waves' results, merged
+      const float l = c.sum();
+      if (lr < cols) {
+        if (lg == 0) {
+          lds.m[wave][lr] = c.m;
+          lds.l[wave][lr] = l;
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+#pragma unroll
+          for (int j = 0; j < VJ; ++j) lds.o[wave][lr][(lg * 4 + e) * VJ + j] = c.o[j][e];
+      }
+      __syncthreads();
+      for (int x = tid - sub * waves * 64; x < cols * (HD / 4) && there && r.n == 1; x += waves * 64) {
+        const int col = x / (HD / 4), d = x % (HD / 4) * 4;
+        float m = -INFINITY, sum = 0.f;
+        for (int w = sub * waves; w < (sub + 1) * waves; ++w) m = fmaxf(m, lds.m[w][col]);
+        const float ref = m == -INFINITY ? 0.f : m;
+        f32x4 o = f32x4{0.f, 0.f, 0.f, 0.f};
+        for (int w = sub * waves; w < (sub + 1) * waves; ++w) {
+          const float f = __builtin_amdgcn_exp2f(lds.m[w][col] - ref);
+          sum += f * lds.l[w][col];
+          o += f * *(const f32x4*)&lds.o[w][col][d];
+        }
+        const int head = hk * a.group.d + col0 + col;
+        if (whole) {
+          const float inv = sum == 0.f ? 0.f : 1.0f / sum;
+          T* dst = (T*)a.o + r.first * a.o_stride + head * HD + d;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) dst[e] = from_f<T>(o[e] * inv);
+          if (a.lse && d == 0) a.lse[(size_t)r.first * a.n_heads + head] = lse_of(m, sum);
+        } else {
+          float* part = single_part(a, HD, share, hb, head_blocks, i0 == 0);
+          *(f32x4*)(part + col * HD + d) = o;
+          if (d == 0) {
+            float* ml = part + min(a.group.d, 16) * HD + 2 * col;
+            ml[0] = m;
+            ml[1] = sum;
+          }
+        }
+      }
+      if (i0 == 0 && hb == 0 && tid == 0 && a.shares) {  // the join's word: the first share, and how many
+        int* word = (int*)a.parts + 2 * b;
+        word[0] = share;
+        word[1] = (before + lead + n - 1) / per - share + 1;
+      }
+    }
+    before += n + lead;
+    at = before;
+    if (!a.shares || at >= end) return;
+    ++b;
+    __syncthreads();
+  }
 }
 
 }  // namespace af

@@ -36,7 +36,7 @@ af_status check_cache(const char* me, const af_paged_kv* kv, int32_t M, int32_t 
   const int64_t cap = (int64_t)kv->max_pages * kv->page_size;
   if (cap > PAGED_MAX_KEYS) return unsupported("a request's pages hold more than 2^30 keys");
   if ((int64_t)M * n_heads >= 1 << 30) return unsupported("M * n_heads is 2^30 or more");
-  if (kv->n_seq * (cap / 32 + 2) > INT_MAX) return unsupported("n_seq * max_pages * page_size / 32 is past 2^31");
+  if (kv->n_seq * (cap / 32 + 8) > INT_MAX) return unsupported("n_seq * max_pages * page_size / 32 is past 2^31");
   if (!aligned(kv->k, 16) || !aligned(kv->v, 16)) return unsupported("need 16-byte aligned k and v");
   *c = PagedCache{kv->k, kv->v, kv->page_table, kv->kv_lens, kv->q_starts, kv->n_pages, __builtin_ctz(kv->page_size),
                   kv->n_kv_heads, kv->n_seq, kv->max_pages, (int)cap, M};
@@ -138,8 +138,8 @@ extern "C" af_status af_op_attention_paged(const af_paged_kv* kv, const void* q,
   a.n_heads = n_heads, a.group = divisor(n_heads / kv->n_kv_heads), a.n_kv_heads = divisor(kv->n_kv_heads);
   a.scale_log2 = (float)(scale * 1.4426950408889634);
   a.window = window ? window : INT_MAX, a.sinks = window ? n_sink : 0;
-  a.parts = (float*)workspace, a.rows_at = p.rows_at;
-  a.shares = p.shares, a.row_splits = p.row_splits;
+  a.parts = (float*)workspace, a.parts_at = p.parts_at, a.rows_at = p.rows_at;
+  a.shares = p.shares, a.single_waves = p.single_waves, a.row_split = p.row_split;
   AF_HIP(launch_attention_paged(kv->dtype, kv->head_dim, a, p, (hipStream_t)hip_stream));
   return AF_OK;
 }

@@ -60,7 +60,8 @@ def test_sizes_that_no_launch_takes():
     refused(UNS, "2^31", lib.af_op_attention_paged, attend_args(d))
     refused(UNS, "2^30", lib.af_op_attention_paged, attend_args(desc(q_starts=P), M=1 << 29))
     refused(UNS, "2^24", lib.af_op_rope_append_paged, append_args(desc(q_starts=P), M=1 << 24))
-    refused(UNS, "launch", lib.af_op_attention_paged, attend_args(desc(n_seq=1 << 23), M=1 << 23))
+    refused(UNS, "launch", lib.af_op_attention_paged,
+            attend_args(desc(n_seq=1 << 23, n_kv_heads=8), M=1 << 23, n_heads=8, q_stride=512, o_stride=512))
 
 
 def test_append_refuses():
