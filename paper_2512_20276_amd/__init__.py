@@ -488,12 +488,12 @@ class PagedKV:
 
     def _rows(self, what: str, t: torch.Tensor, M: int, n_heads: int) -> int:
         """Elements between the rows of ``t`` [M, n_heads, head_dim], whose heads lie side by side."""
-        hd = self.head_dim
-        if (t.dtype is not self.dtype or t.get_device() != self.device or t.shape != (M, n_heads, hd) or t.stride(2) != 1
-                or (n_heads > 1 and t.stride(1) != hd)):
+        hd, strides = self.head_dim, t.stride()
+        if (t.dtype is not self.dtype or t.shape != (M, n_heads, hd) or t.get_device() != self.device or strides[2] != 1
+                or (n_heads > 1 and strides[1] != hd)):
             raise ValueError(f"{what} must be a {self.dtype} tensor of shape {(M, n_heads, hd)} with the heads of a row side "
                              f"by side, on the cache's device, got {t.dtype} {tuple(t.shape)} {t.stride()} on {t.device}")
-        return t.stride(0) if M > 1 else n_heads * hd
+        return strides[0] if M > 1 else n_heads * hd
 
 
 def op_rope_append_paged(kv: PagedKV, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, q_out: torch.Tensor,

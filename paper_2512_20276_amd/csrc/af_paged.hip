@@ -9,9 +9,22 @@ namespace af {
 // the whole turns are taken off, so that far positions keep their angle (an angle of 10^5 in 32 bits is off by
 // 0.004).  The row's HD/2 sines and cosines are computed once, by as many threads, while the row's queries, keys
 // and values are on their way, and read by all heads from LDS.  A thread rotates 8 pairs of a head at a time.
+// Eight elements whose address is a multiple of 16 bytes.
+template <typename T>
+struct Chunk8;
+template <>
+struct Chunk8<bf16> {
+  typedef bf16x8 type;
+};
+template <>
+struct Chunk8<float> {
+  typedef f32x8 type __attribute__((aligned(16)));
+};
+
 template <typename T, int HD>
 __global__ __launch_bounds__(256) void rope_append_kernel(AppendArgs a) {
   constexpr int HALF = HD / 2, PT = HALF / 8;  // threads of a head
+  typedef typename Chunk8<T>::type V8;
   __shared__ float cs[2][HALF];
   const int row = blockIdx.x, tid = threadIdx.x;
   const int b = request_of_row(a.c, row);
@@ -41,24 +54,20 @@ __global__ __launch_bounds__(256) void rope_append_kernel(AppendArgs a) {
     const T* src = key ? (const T*)a.k + row * a.k_stride + (h - a.n_heads) * HD : (const T*)a.q + row * a.q_stride + h * HD;
     T* dst = key ? (T*)c.k + (cell + (h - a.n_heads) * head_rows) * HD : (T*)a.q_out + row * a.q_out_stride + h * HD;
     if (key && !write) continue;
-    T x[8], y[8];
-    load8(src + j, x);
-    load8(src + HALF + j, y);
+    V8 x = *(const V8*)(src + j), y = *(const V8*)(src + HALF + j);
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
       const float u = to_f(x[e]), w = to_f(y[e]), co = cs[0][j + e], si = cs[1][j + e];
       x[e] = from_f<T>(u * co - w * si);
       y[e] = from_f<T>(w * co + u * si);
     }
-    store8(dst + j, x);
-    store8(dst + HALF + j, y);
+    *(V8*)(dst + j) = x;
+    *(V8*)(dst + HALF + j) = y;
   }
   if (!write) return;
   for (int i = tid; i < c.n_kv_heads * (HD / 8); i += 256) {
     const int h = i / (HD / 8), d = i % (HD / 8) * 8;
-    T x[8];
-    load8((const T*)a.v + row * a.v_stride + h * HD + d, x);
-    store8((T*)c.v + (cell + h * head_rows) * HD + d, x);
+    *(V8*)((T*)c.v + (cell + h * head_rows) * HD + d) = *(const V8*)((const T*)a.v + row * a.v_stride + h * HD + d);
   }
 }
 

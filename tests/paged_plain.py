@@ -61,9 +61,10 @@ class Step:
         """Rotated q and k in 64 bits and the bound of each result's error.
 
         The angle, in half turns, is rounded to fp32 once (2^-25 of a half turn: pi 2^-25), after a product in 64 bits
-        (3 2^-53 of the whole angle: its own rounding and the frequency's).  A sine or cosine is within 4 ulp
-        (2^-22).  So each is off by less than 2^-22 + pi 2^-25 + 3 2^-53 angle < 2^-21 - 2^-23 + ..; two products and their sum add
-        2 U32 of |x| + |y| at most: (|x| + |y|) (2^-21 + 3 2^-53 angle), and the result's rounding."""
+        (its own rounding, 2^-53 of the whole angle, and the frequency's: two powers within an ulp's half and a little, their
+        product and a division by 2 pi, which is rounded itself: 6 2^-53 in all).  A sine or cosine is within 4 ulp
+        (2^-22).  So each is off by less than 2^-22 + pi 2^-25 + 6 2^-53 angle < 2^-21 - 2^-23 + ..; two products and their sum add
+        2 U32 of |x| + |y| at most: (|x| + |y|) (2^-21 + 6 2^-53 angle), and the result's rounding."""
         half = self.hd // 2
         pos = torch.zeros(self.M, 1, dtype=torch.float64)
         if positions is None:
@@ -79,7 +80,7 @@ class Step:
             a, b = x[..., :half].double(), x[..., half:].double()
             co, si = angle.cos()[:, None], angle.sin()[:, None]
             y = torch.cat([a * co - b * si, b * co + a * si], dim=-1)
-            each = (a.abs() + b.abs()) * (2.0 ** -21 + 3 * 2.0 ** -53 * angle.abs()[:, None])
+            each = (a.abs() + b.abs()) * (2.0 ** -21 + 6 * 2.0 ** -53 * angle.abs()[:, None])
             each = torch.cat([each, each], dim=-1)
             out.append((y, each + HALF_STEP[self.dtype] * (y.abs() + each)))
         return out

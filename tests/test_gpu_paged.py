@@ -156,7 +156,8 @@ def test_several_rows(dtype, hd, Hkv, group, page, requests):
 
 
 @pytest.mark.parametrize("dtype", [BF16, F32])
-@pytest.mark.parametrize("requests", [[(2, 4000)], [(40, 3000), (1, 2500), (3, 700)], [(17, 2100)] * 3])
+@pytest.mark.parametrize("requests", [[(2, 4000)], [(40, 3000), (1, 2500), (3, 700)], [(17, 2100)] * 3, [(700, 1500), (1, 3000)],
+                                      [(2, 2100), (2, 40)]])
 def test_chunks_on_long_caches(dtype, requests):
     """Few rows and many keys: the keys are split and joined."""
     check_attend(Step(requests, 2, 4, 128, 32, dtype))
@@ -170,6 +171,31 @@ def test_several_rows_with_a_window(window, sinks, hd, group, dtype):
 
 def test_window_over_chunks_that_are_split():
     check_attend(Step([(20, 3000), (1, 2900)], 1, 4, 128, 16), window=1700, sinks=40)
+
+
+@pytest.mark.parametrize("n_seq,Hkv,group,hd,dtype", [(701, 3, 2, 64, BF16), (351, 3, 4, 128, F32), (2101, 1, 1, 64, F32)])
+@pytest.mark.parametrize("single", [True, False])
+def test_short_caches_of_many_requests(n_seq, Hkv, group, hd, dtype, single):
+    """A request's key head on one, two or four waves, with waves left over in the last workgroup."""
+    requests = [(1 if single else (1, 1, 0, 2)[i % 4], 1 + (i * 31) % (100 if i % 9 else 3)) for i in range(n_seq)]
+    requests = [(n, max(n, length)) for n, length in requests]
+    check_attend(Step(requests, Hkv, group, hd, 16, dtype, single=single))
+
+
+def test_many_requests_of_long_caches():
+    """More requests than a wave has lanes, whose keys are split: single rows, chunks, rows of nobody."""
+    requests = [((0, 1, 1, 2, 9)[i % 5], 9 + (i * 37) % 90 + (1500 if i % 23 == 0 else 0)) for i in range(131)]
+    check_attend(Step(requests, 1, 4, 64, 16, before=2, behind=5))
+    check_attend(Step(requests, 1, 4, 64, 16, before=2, behind=5), window=700, sinks=9)
+
+
+def test_the_same_inputs_give_the_same_bits():
+    for requests, single in (([(1, 2000), (1, 5), (1, 900)], True), ([(30, 2000), (1, 1500), (9, 60)], False)):
+        s = Step(requests, 2, 4, 128, 16, single=single)
+        first, lse = attend(s)
+        for _ in range(3):
+            again, more = attend(s)
+            assert torch.equal(first, again) and torch.equal(lse, more)
 
 
 def test_many_requests():

@@ -96,7 +96,7 @@ def test_attention_refuses():
         refused(INV, f"rows of {n}", fn, attend_args(d, **{n + "_stride": 255}))
     refused(INV, "window", fn, attend_args(d, window=-1))
     refused(INV, "n_sink", fn, attend_args(d, n_sink=-1))
-    for scale in (math.inf, math.nan):
+    for scale in (math.inf, math.nan, 3e38):
         refused(INV, "scale", fn, attend_args(d, scale=scale))
     refused(INV, "aligned", fn, attend_args(d, lse=P + 2))
     long = desc(max_pages=100)
