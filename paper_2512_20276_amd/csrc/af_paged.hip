@@ -228,7 +228,9 @@ bool paged_plan(int dtype, int head_dim, int n_kv_heads, int n_heads, int n_seq,
   const long most_tiles = (cap + KEY_TILE - 1) / KEY_TILE + 1;  // of a request's keys
   long floats = 0, single_grid = 0, row_grid = 0, join_singles = 0, join_rows = 0;
   *p = PagedPlan{};
-  if (cap > DIRECT_KEYS) {
+  // One request of a step of several rows is a prompt or a chunk of one; should it have a single row all the same, that
+  // is not split, which saves the others the join (4 us).
+  if (cap > DIRECT_KEYS && (single || n_seq > 1 || M == 1)) {
     const long shares = std::min((SINGLE_GRID + head_blocks - 1) / head_blocks, n_seq * (most_tiles + PIECE_TILES) / SHARE_TILES + 1);
     p->shares = (int)shares;
     single_grid = shares * head_blocks;

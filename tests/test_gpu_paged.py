@@ -169,6 +169,15 @@ def test_several_rows_with_a_window(window, sinks, hd, group, dtype):
     check_attend(Step([(150, 150), (70, 400), (1, 200), (3, 90)], 2, group, hd, 16, dtype), window=window, sinks=sinks)
 
 
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_one_request_of_a_packed_step(dtype):
+    """A prompt, and a single row with rows of nobody around it, on a long cache."""
+    check_attend(Step([(50, 1900)], 2, 4, 64, 16, dtype, before=1, behind=2))
+    check_attend(Step([(1, 1900)], 2, 4, 64, 16, dtype, before=1, behind=2))
+    check_attend(Step([(1, 1900)], 2, 4, 64, 16, dtype))
+    check_attend(Step([(0, 1900)], 2, 4, 64, 16, dtype, behind=2))
+
+
 def test_window_over_chunks_that_are_split():
     check_attend(Step([(20, 3000), (1, 2900)], 1, 4, 128, 16), window=1700, sinks=40)
 
