@@ -52,21 +52,22 @@ struct PagedAttnArgs {
   long parts_at, rows_at;  // floats before those of shares (the join's words), and before those of tiles of rows
   int shares;          // requests with a single row: shares of a key head's keys, 0: a workgroup for each request
   int single_waves;    // and its waves for each, 1, 2 or 4
-  int row_split;       // other requests: a tile's keys may be split
 };
 // A partial result: outputs of `cols` columns, then a maximum and a sum for each, in whole chunks of 16 bytes.
 __host__ __device__ inline size_t paged_part_floats(int cols, int hd) { return ((size_t)cols * (hd + 2) + 3) / 4 * 4; }
-// Tiles of rows: columns and keys of one, which go by the type, and the fewest keys of a part of them.
+// Tiles of rows: columns and keys of one, and the fewest key tiles of a part, which go by the type.
 template <typename T>
 constexpr int ROW_TILE = sizeof(T) == 2 ? 128 : 64;
 template <typename T>
 constexpr int ROW_KEYS = sizeof(T) == 2 ? 64 : 32;
-constexpr int SPLIT_TILES = 16;
-constexpr int ROW_GRID = 512;  // workgroups that a split of tiles of rows is to give
+template <typename T>
+constexpr int SPLIT_TILES = sizeof(T) == 2 ? 8 : 4;
+constexpr int ROW_GRID = 512;  // workgroups that tiles of rows and their parts are to give: as many as the GPU holds at once
 
 // How a call of these sizes is launched, and its workspace.
 struct PagedPlan {
-  int shares, single_waves, row_split;
+  int shares, single_waves;
+  bool row_split;                  // the keys of tiles of rows may be split
   long parts_at, rows_at, floats;  // floats of workspace before shares, before tiles of rows, in all
   int single_grid, row_grid;       // workgroups of single rows, of tiles of rows
   int tile_grid;                   // of these, as many as there can be tiles

@@ -164,59 +164,63 @@ __device__ __forceinline__ void join_single(const PagedAttnArgs& a, int b, int h
   if (lse && tid == 0) *lse = lse_of(m, total);
 }
 
-constexpr int JOIN_THREADS = 8, JOIN_COLS = 256 / JOIN_THREADS;
-// 32 columns of a tile of rows, by a workgroup: 8 threads a column.
+// Tiles of rows that were split, JOIN_COLS columns at a time: a fixed number of workgroups that go on while there are
+// any, since only the lengths tell how many there are.
+constexpr int JOIN_COLS = 8;
+constexpr int JOIN_GRID = 1024;
 template <typename T, int HD>
-__device__ __forceinline__ void join_rows(const PagedAttnArgs& a, int item, int col_block) {
-  constexpr int DT = HD / JOIN_THREADS, COLS = ROW_TILE<T>;
-  const int tile = quotient(item, a.n_kv_heads), hk = remainder(item, a.n_kv_heads, tile);
-  const RowTile<ROW_KEYS<T>> t = row_tile<ROW_KEYS<T>, COLS, true>(a, tile);
-  if (t.b < 0) return;
-  const int n = t.splits;
-  const int col = col_block * JOIN_COLS + threadIdx.x / JOIN_THREADS, d = threadIdx.x % JOIN_THREADS * DT;
-  if (n == 1 || col >= t.cols) return;
-  float m = -INFINITY, l = 0.f, o[DT] = {};
-  for (int i0 = 0; i0 < n; i0 += 4) {
-    float pm[4], pl[4], po[4][DT];
+__device__ __forceinline__ void join_rows(const PagedAttnArgs& a, int x, int grid) {
+  constexpr int THREADS = 256 / JOIN_COLS, DT = HD / THREADS, COLS = ROW_TILE<T>, BLOCKS = COLS / JOIN_COLS, AHEAD = 8;
+  RowTiles<T, true> tiles;
+  tiles.init(a);
+  for (;; x += grid) {
+    const int item = x / BLOCKS, tile = quotient(item, a.n_kv_heads), hk = remainder(item, a.n_kv_heads, tile);
+    const RowTile<ROW_KEYS<T>> t = tiles.template find<true>(a, tile);
+    if (t.b < 0) return;
+    const int n = t.splits, col = x % BLOCKS * JOIN_COLS + threadIdx.x / THREADS, d = threadIdx.x % THREADS * DT;
+    if (n == 1 || col >= t.cols) continue;
+    float m = -INFINITY, l = 0.f, o[DT] = {};
+    for (int i0 = 0; i0 < n; i0 += AHEAD) {  // so many parts on their way at once
+      float pm[AHEAD], pl[AHEAD], po[AHEAD][DT], up = m;
 #pragma unroll
-    for (int u = 0; u < 4; ++u) {
-      const float* part = row_part(a, COLS, HD, t.part0 + min(i0 + u, n - 1), hk);
-      pm[u] = i0 + u < n ? part[COLS * HD + 2 * col] : -INFINITY;
-      pl[u] = part[COLS * HD + 2 * col + 1];
-      __builtin_memcpy(po[u], __builtin_assume_aligned(part + col * HD + d, 16), sizeof(po[u]));
+      for (int u = 0; u < AHEAD; ++u) {
+        pm[u] = -INFINITY;
+        if (i0 + u >= n) continue;
+        const float* part = row_part(a, COLS, HD, t.part0 + i0 + u, hk);
+        pm[u] = part[COLS * HD + 2 * col];
+        pl[u] = part[COLS * HD + 2 * col + 1];
+        __builtin_memcpy(po[u], __builtin_assume_aligned(part + col * HD + d, DT * 4), sizeof(po[u]));
+      }
+#pragma unroll
+      for (int u = 0; u < AHEAD; ++u) up = fmaxf(up, pm[u]);
+      const float ref = up == -INFINITY ? 0.f : up, f = exp2f(m - ref);
+      l *= f;
+#pragma unroll
+      for (int e = 0; e < DT; ++e) o[e] *= f;
+      m = up;
+#pragma unroll
+      for (int u = 0; u < AHEAD; ++u) {
+        if (i0 + u >= n) continue;
+        const float w = exp2f(pm[u] - ref);
+        l += w * pl[u];
+#pragma unroll
+        for (int e = 0; e < DT; ++e) o[e] += w * po[u][e];
+      }
     }
-    const float up = fmaxf(fmaxf(fmaxf(pm[0], pm[1]), fmaxf(pm[2], pm[3])), m), ref = up == -INFINITY ? 0.f : up;
-    const float f = exp2f(m - ref);
-    l *= f;
+    const float inv = l == 0.f ? 0.f : 1.0f / l;
+    const int i_row = quotient(t.col0 + col, a.group), row = t.r.first + i_row, head = hk * a.group.d + remainder(t.col0 + col, a.group, i_row);
+    T* dst = (T*)a.o + row * a.o_stride + head * HD + d;
 #pragma unroll
-    for (int e = 0; e < DT; ++e) o[e] *= f;
-    m = up;
-#pragma unroll
-    for (int u = 0; u < 4; ++u) {
-      if (i0 + u >= n) break;
-      const float w = exp2f(pm[u] - ref);
-      l += w * pl[u];
-#pragma unroll
-      for (int e = 0; e < DT; ++e) o[e] += w * po[u][e];
-    }
+    for (int e = 0; e < DT; ++e) dst[e] = from_f<T>(o[e] * inv);
+    if (a.lse && d == 0) a.lse[(size_t)row * a.n_heads + head] = lse_of(m, l);
   }
-  const float inv = l == 0.f ? 0.f : 1.0f / l;
-  const int i_row = quotient(t.col0 + col, a.group), row = t.r.first + i_row, head = hk * a.group.d + remainder(t.col0 + col, a.group, i_row);
-  T* dst = (T*)a.o + row * a.o_stride + head * HD + d;
-#pragma unroll
-  for (int e = 0; e < DT; ++e) dst[e] = from_f<T>(o[e] * inv);
-  if (a.lse && d == 0) a.lse[(size_t)row * a.n_heads + head] = lse_of(m, l);
 }
 
 template <typename T, int HD>
 __global__ __launch_bounds__(256) void join_kernel(PagedAttnArgs a, int singles) {
-  const int i = blockIdx.x;
-  if (i < singles) {
-    join_single<T, HD>(a, i / a.n_heads, i % a.n_heads);
-  } else {
-    const int blocks = ROW_TILE<T> / JOIN_COLS;
-    join_rows<T, HD>(a, (i - singles) / blocks, (i - singles) % blocks);
-  }
+  const int x = blockIdx.x;
+  if (x < singles) join_single<T, HD>(a, x / a.n_heads, x % a.n_heads);
+  else join_rows<T, HD>(a, x - singles, gridDim.x - singles);
 }
 
 // ------------------------------------------------------------------ launch
@@ -245,7 +249,7 @@ bool paged_plan(int dtype, int head_dim, int n_kv_heads, int n_heads, int n_seq,
   }
   p->rows_at = floats;
   const int row_tile = dtype == AF_BF16 ? ROW_TILE<bf16> : ROW_TILE<float>;
-  const int split_keys = SPLIT_TILES * (dtype == AF_BF16 ? ROW_KEYS<bf16> : ROW_KEYS<float>);
+  const int split_keys = dtype == AF_BF16 ? SPLIT_TILES<bf16> * ROW_KEYS<bf16> : SPLIT_TILES<float> * ROW_KEYS<float>;
   if (!single) {
     const long columns = (long)M * group, tiles = columns / row_tile + std::min(n_seq, M / 2);  // at most so many
     row_grid = tiles * n_kv_heads;
@@ -254,7 +258,7 @@ bool paged_plan(int dtype, int head_dim, int n_kv_heads, int n_heads, int n_seq,
     const long sure = (long)std::max(M - n_seq, 0) * group / row_tile * n_kv_heads;
     if (cap > split_keys && sure <= ROW_GRID / 2) {
       p->row_split = 1;
-      join_rows = tiles * n_kv_heads * (row_tile / JOIN_COLS);
+      join_rows = std::min(tiles * n_kv_heads * (row_tile / JOIN_COLS), (long)JOIN_GRID);
       // Tiles in two parts or more have fewer than twice as many as their keys are parts long: 2 ROW_GRID in all (and a little
       // for the sum's rounding).
       const long most_parts = std::min(2L * ROW_GRID + 64, row_grid * (cap / split_keys + 2));

@@ -258,6 +258,17 @@ __device__ __forceinline__ int wave_prefix(int v, int& total) {
   return x - v;
 }
 
+// The same sum of floats, in one order.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ float plus_dpp(float x) {
+  return x + __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(x), CTRL, ROWS, 0xf, false));
+}
+__device__ __forceinline__ float wave_total(float x) {
+  x = plus_dpp<0x118, 0xf>(plus_dpp<0x114, 0xf>(plus_dpp<0x112, 0xf>(plus_dpp<0x111, 0xf>(x))));
+  x = plus_dpp<0x143, 0xc>(plus_dpp<0x142, 0xa>(x));
+  return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(x), 63));
+}
+
 // ------------------------------------------------------------------ tiles of rows
 // The rows of a request with several, each with the heads that share a key head, are columns: column x is head x % group
 // of row x / group, so that a tile of columns spans few positions.
@@ -273,74 +284,103 @@ struct RowTile {
   int from, end;        // its key tiles
   int part0;            // partial results of all tiles before this one's
 };
-// Where few rows meet many keys the keys are cut into parts of a length that gives about ROW_GRID workgroups (of
-// SPLIT_TILES key tiles at least), about the same for all requests.  Every tile of a request is given as many parts as its
-// last one, whose rows see the most keys, takes; tiles that take fewer leave the others idle, and the last part takes
-// what is left.  A request's last tile is begun first.  Workgroup `at` of a key head: its tile and part; JOIN: tile `at`, part 0.
-// The requests are read once by the lanes of a wave, a second time only where they are more than 64.
-template <int TK, int COLS, bool JOIN = false>
-__device__ __forceinline__ RowTile<TK> row_tile(const PagedAttnArgs& a, int at) {
-  const int lane = threadIdx.x & 63;
-  RowTile<TK> t;
-  t.b = -1;
-  Request r{0, 0, 0};
-  int n = 0, most = 0;  // tiles of the lane's request, key tiles of its last one
-  const auto read = [&](int b0) {
-    n = 0;
-    if (b0 + lane < a.c.n_seq) {
-      r = request_at(a.c, b0 + lane);
-      if (r.n > 1) n = (r.n * a.group.d + COLS - 1) / COLS;
+// Where few rows meet many keys the keys are cut into parts of a length that gives about as many workgroups as the GPU
+// holds at once (of SPLIT_TILES<T> key tiles at least), about the same for all requests.  Every tile of a request is given
+// as many parts as its last one, whose rows see the most keys, takes; tiles that take fewer leave the others idle, and the
+// last part takes what is left.  A request's last tile is begun first.
+// The requests are read once by the lanes of a wave, again only where they are more than 64.
+template <typename T, bool SPLIT>
+struct RowTiles {
+  static constexpr int TK = ROW_KEYS<T>, COLS = ROW_TILE<T>;
+  Request r;
+  int n, most;   // tiles of the lane's request, key tiles of its last one
+  int per;       // key tiles of a part
+
+  __device__ __forceinline__ void read(const PagedAttnArgs& a, int b0) {
+    const int b = b0 + (threadIdx.x & 63);
+    n = 0, most = 0;
+    r = Request{0, 0, 0};
+    if (b < a.c.n_seq) r = request_at(a.c, b);
+    if (r.n > 1) {
+      n = (r.n * a.group.d + COLS - 1) / COLS;
+      if (SPLIT) most = key_tiles<TK>(a, r.len - min(r.n, quotient(COLS - 1, a.group) + 1), r.len - 1).n;
     }
-    if (a.row_split) most = key_tiles<TK>(a, r.len - min(r.n, quotient(COLS - 1, a.group) + 1), r.len - 1).n;
-  };
-  int per = 1 << 30;  // key tiles of a part
-  if (!a.row_split && a.c.n_seq <= 64) {
-    read(0);
-  } else {
-    float work = 0.f;
+  }
+  __device__ __forceinline__ void init(const PagedAttnArgs& a) {
+    per = 1 << 30;
+    if (a.c.n_seq <= 64) read(a, 0);
+    if constexpr (!SPLIT) return;
+    // What a workgroup would take if all tiles were split; then, of the requests that are split, what it takes if the
+    // tiles of the others have a workgroup each.  A split tile's parts are half a part more than its keys, on average.  Single
+    // rows beside them find an eighth of the places free (with none, four chunks and 28 single rows took 53 us instead of 43).
+    float share = 0.f;
+#pragma unroll 1
+    for (int turn = 0; turn < 2; ++turn) {
+      float work = 0.f, whole = 0.f;
+      bool singles = false;
+      for (int b0 = 0; b0 < a.c.n_seq; b0 += 64) {
+        if (a.c.n_seq > 64) read(a, b0);
+        float w = (float)n * (float)most, x = 0.5f * n;
+        if ((float)most <= share) w = 0.f, x = (float)n;
+        work += wave_total(w);
+        whole += wave_total(x);
+        singles |= __any(r.n == 1);
+      }
+      const float places = singles ? ROW_GRID * 7 / 8 : ROW_GRID;
+      share = work * a.c.n_kv_heads / fmaxf(places - whole * a.c.n_kv_heads, ROW_GRID / 8);
+    }
+    per = scalar(max((int)fminf(share, 1e9f) + 1, SPLIT_TILES<T>));  // (1e9: more than any tile has)
+  }
+  // Workgroup `at` of a key head: its tile and part.  JOIN: tile `at` of those that are split, part 0.
+  template <bool JOIN>
+  __device__ __forceinline__ RowTile<TK> find(const PagedAttnArgs& a, int at) {
+    RowTile<TK> t;
+    t.b = -1;
+    int before = 0, parts_before = 0, each = 1, length = per;
     for (int b0 = 0; b0 < a.c.n_seq; b0 += 64) {
-      read(b0);
-      float w = (float)n * (float)most;
-#pragma unroll
-      for (int d = 1; d < 64; d <<= 1) w += __shfl_xor(w, d);
-      work += w;
+      if (a.c.n_seq > 64) read(a, b0);
+      const int parts = SPLIT ? max((most + per - 1) / per, 1) : 1;
+      const int weight = JOIN ? (parts > 1 ? n : 0) : n * parts;
+      int all, all_parts = 0;
+      const int prefix = wave_prefix(weight, all), of_parts = JOIN ? wave_prefix(n * parts, all_parts) : 0;
+      const unsigned long long past = __ballot(before + prefix + weight > at);
+      if (past) {
+        const int l = __builtin_ctzll(past);
+        t.b = b0 + l;
+        t.r = Request{__builtin_amdgcn_readlane(r.first, l), __builtin_amdgcn_readlane(r.n, l), __builtin_amdgcn_readlane(r.len, l)};
+        each = __builtin_amdgcn_readlane(parts, l);
+        if (each > 1) length = (__builtin_amdgcn_readlane(most, l) + each - 1) / each;
+        const int within = at - before - __builtin_amdgcn_readlane(prefix, l);
+        const int tile = JOIN || !SPLIT || each == 1 ? within : within / each;
+        t.split = JOIN ? 0 : within - tile * each;
+        t.part0 = JOIN ? parts_before + __builtin_amdgcn_readlane(of_parts, l) + within * each : at - t.split;
+        t.col0 = (__builtin_amdgcn_readlane(n, l) - 1 - tile) * COLS;
+        break;
+      }
+      before += all;
+      parts_before += all_parts;
     }
-    // (more than any tile has if work is past what fits)
-    if (a.row_split) per = scalar(max((int)fminf(work * a.c.n_kv_heads * (1.0f / ROW_GRID), 1e9f) + 1, SPLIT_TILES));
-  }
-  int before = 0, parts_before = 0, each = 1;
-  for (int b0 = 0; b0 < a.c.n_seq; b0 += 64) {
-    if (a.c.n_seq > 64) read(b0);
-    const int parts = a.row_split ? max((most + per - 1) / per, 1) : 1;
-    int all, all_parts = 0;
-    const int prefix = wave_prefix(JOIN ? n : n * parts, all), of_parts = JOIN ? wave_prefix(n * parts, all_parts) : 0;
-    const unsigned long long past = __ballot(before + prefix + (JOIN ? n : n * parts) > at);
-    if (past) {
-      const int l = __builtin_ctzll(past);
-      t.b = b0 + l;
-      t.r = Request{__builtin_amdgcn_readlane(r.first, l), __builtin_amdgcn_readlane(r.n, l), __builtin_amdgcn_readlane(r.len, l)};
-      each = __builtin_amdgcn_readlane(parts, l);
-      if (each > 1) per = (__builtin_amdgcn_readlane(most, l) + each - 1) / each;
-      const int within = at - before - __builtin_amdgcn_readlane(prefix, l);
-      const int tile = JOIN || each == 1 ? within : within / each;
-      t.split = JOIN ? 0 : within - tile * each;
-      t.part0 = JOIN ? parts_before + __builtin_amdgcn_readlane(of_parts, l) + within * each : at - t.split;
-      t.col0 = (__builtin_amdgcn_readlane(n, l) - 1 - tile) * COLS;
-      break;
+    if (t.b < 0) return t;
+    t.cols = min(COLS, t.r.n * a.group.d - t.col0);
+    t.lowest = t.r.len - t.r.n + quotient(t.col0, a.group);
+    t.highest = t.r.len - t.r.n + quotient(t.col0 + t.cols - 1, a.group);
+    t.keys = key_tiles<TK>(a, t.lowest, t.highest);
+    if constexpr (!SPLIT) {
+      t.split = 0, t.splits = 1, t.from = 0, t.end = t.keys.n;
+      return t;
     }
-    before += all;
-    parts_before += all_parts;
+    t.splits = each == 1 ? 1 : max(min((t.keys.n + length - 1) / length, each), 1);
+    t.from = t.split * length;
+    t.end = t.split == t.splits - 1 ? t.keys.n : t.from + length;
+    if (t.split >= t.splits) t.b = -1;
+    return t;
   }
-  if (t.b < 0) return t;
-  t.cols = min(COLS, t.r.n * a.group.d - t.col0);
-  t.lowest = t.r.len - t.r.n + quotient(t.col0, a.group);
-  t.highest = t.r.len - t.r.n + quotient(t.col0 + t.cols - 1, a.group);
-  t.keys = key_tiles<TK>(a, t.lowest, t.highest);
-  t.splits = each == 1 ? 1 : max(min((t.keys.n + per - 1) / per, each), 1);
-  t.from = t.split * per;
-  t.end = t.split == t.splits - 1 ? t.keys.n : t.from + per;
-  if (t.split >= t.splits) t.b = -1;
-  return t;
+};
+template <typename T, bool SPLIT>
+__device__ __forceinline__ RowTile<ROW_KEYS<T>> row_tile(const PagedAttnArgs& a, int at) {
+  RowTiles<T, SPLIT> tiles;
+  tiles.init(a);
+  return tiles.template find<false>(a, at);
 }
 // Partial result of one part: cols x HD outputs, then a maximum and a sum for each column.
 __device__ __forceinline__ float* row_part(const PagedAttnArgs& a, int cols, int hd, int part, int hk) {

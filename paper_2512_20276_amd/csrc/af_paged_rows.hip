@@ -35,13 +35,13 @@ struct PageTiles {
 // probabilities go up to 2^8 instead of 1, with the same relative precision.
 // A probability is rounded to bf16 once (2^-8 of it at most): a remainder as in attend_tile would cost a third
 // more matrix instructions, which bound this kernel.  Sums are of the unrounded ones.
-template <int HD>
+template <int HD, bool SPLIT>
 __device__ __forceinline__ void attend_tiles(const PagedAttnArgs& a, int block, char* smem, int& odd_tile) {
   typedef PageTiles<HD> L;
   constexpr int TK = L::KEYS, COLS = ROW_TILE<bf16>, KST = HD / 16, OB = HD / 32;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), ln = lane & 31, h = lane >> 5;
   const int at = quotient(block, a.n_kv_heads), hk = remainder(block, a.n_kv_heads, at);
-  const RowTile<TK> t = row_tile<TK, COLS>(a, at);
+  const RowTile<TK> t = row_tile<bf16, SPLIT>(a, at);
   if (t.b < 0) return;
 
   // ---- the wave's columns (those past the last one repeat it and are not stored)
@@ -320,7 +320,7 @@ __device__ __forceinline__ void attend_tiles(const PagedAttnArgs& a, int block, 
 
   l += __shfl_xor(l, 32);
   const bool real = w0 + ln < t.cols;
-  if (t.splits == 1) {
+  if (!SPLIT || t.splits == 1) {
     const float inv = l == 0.f ? 0.f : 1.0f / l;
     // a lane has four of every eight dimensions, its other half the others: halves are exchanged so that each has eight in a row
     bf16* dst = (bf16*)a.o + row * a.o_stride + head * HD + 8 * h;
@@ -357,14 +357,14 @@ __device__ __forceinline__ void attend_tiles(const PagedAttnArgs& a, int block, 
 
 // fp32.  Four waves, 16 columns each, that read keys and values themselves: the matrix instructions of this
 // type, a sixteenth as fast, bound it.
-template <int HD>
+template <int HD, bool SPLIT>
 __device__ __forceinline__ void attend_rows(const PagedAttnArgs& a, int block) {
   typedef Columns<float, HD> C;
   constexpr int VJ = C::VJ, TK = KEY_TILE, COLS = ROW_TILE<float>;
   static_assert(ROW_KEYS<float> == KEY_TILE && ROW_TILE<float> == 64, "four waves of 16 columns");
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, lr = lane & 15, lg = lane >> 4;
   const int at = quotient(block, a.n_kv_heads), hk = remainder(block, a.n_kv_heads, at);
-  const RowTile<TK> t = row_tile<TK, COLS>(a, at);
+  const RowTile<TK> t = row_tile<float, SPLIT>(a, at);
   if (t.b < 0) return;
   const int w0 = wave * 16;
   if (w0 >= t.cols) return;
@@ -375,14 +375,15 @@ __device__ __forceinline__ void attend_rows(const PagedAttnArgs& a, int block) {
   C c;
   c.clear();
   c.load_q((const float*)a.q + row * a.q_stride + head * HD);
+  int entry = t.from < t.end ? page_entry<TK>(a.c, t.b, t.keys.key(t.from)) : -1;
   for (int i = t.from; i < t.end; ++i) {
-    const int j0 = t.keys.key(i);
-    if (none_see(a, lowest, highest, j0, TK)) continue;
-    attend_tile<float, HD, true>(a, hk, j0, page_of<TK>(a.c, t.b, j0), p, lowest, highest, c);
+    const int j0 = t.keys.key(i), page = page_of_entry<TK>(a.c, j0, entry);
+    if (i + 1 < t.end) entry = page_entry<TK>(a.c, t.b, t.keys.key(i + 1));
+    if (!none_see(a, lowest, highest, j0, TK)) attend_tile<float, HD, true>(a, hk, j0, page, p, lowest, highest, c);
   }
   const float l = c.sum();
   if (w0 + lr >= t.cols) return;
-  if (t.splits == 1) {
+  if (!SPLIT || t.splits == 1) {
     const float inv = l == 0.f ? 0.f : 1.0f / l;
     float* dst = (float*)a.o + row * a.o_stride + head * HD + lg * 4 * VJ;
 #pragma unroll
@@ -407,7 +408,7 @@ __device__ __forceinline__ void attend_rows(const PagedAttnArgs& a, int block) {
 // alone, fill the places that they leave.  (Alternating in eights, a prompt of 4096 rows without any single row took
 // 188 us instead of 159, four chunks with 28 single rows 56 instead of 45: the tiles began out of their order.)
 // Workgroups of tiles beyond `tiles`, which are there if many keys are split, come last: most have nothing to do.
-template <typename T, int HD>
+template <typename T, int HD, bool SPLIT>
 __global__ __launch_bounds__(256, 2) void attend_step_kernel(PagedAttnArgs a, int tiles, int singles) {
   const int x = blockIdx.x;
   const bool single = x >= tiles && x < tiles + singles;
@@ -417,17 +418,19 @@ __global__ __launch_bounds__(256, 2) void attend_step_kernel(PagedAttnArgs a, in
     __shared__ int odd_tile;  // the last tile, counted from 1, that held values that are not finite
     static_assert(sizeof(SingleLds<HD>) <= sizeof(smem), "one workgroup's LDS");
     if (single) attend_single<T, HD>(a, block, *(SingleLds<HD>*)smem);
-    else attend_tiles<HD>(a, block, smem, odd_tile);
+    else attend_tiles<HD, SPLIT>(a, block, smem, odd_tile);
   } else {
     __shared__ __attribute__((aligned(16))) SingleLds<HD> lds;
     if (single) attend_single<T, HD>(a, block, lds);
-    else attend_rows<HD>(a, block);
+    else attend_rows<HD, SPLIT>(a, block);
   }
 }
 
 template <typename T, int HD>
 static void step_launch(const PagedAttnArgs& a, const PagedPlan& p, hipStream_t s) {
-  hipLaunchKernelGGL((attend_step_kernel<T, HD>), dim3(p.row_grid + p.single_grid), dim3(256), 0, s, a, p.tile_grid, p.single_grid);
+  const dim3 grid(p.row_grid + p.single_grid), block(256);
+  if (p.row_split) hipLaunchKernelGGL((attend_step_kernel<T, HD, true>), grid, block, 0, s, a, p.tile_grid, p.single_grid);
+  else hipLaunchKernelGGL((attend_step_kernel<T, HD, false>), grid, block, 0, s, a, p.tile_grid, p.single_grid);
 }
 
 hipError_t launch_paged_rows(int dtype, int head_dim, const PagedAttnArgs& a, const PagedPlan& p, hipStream_t s) {
