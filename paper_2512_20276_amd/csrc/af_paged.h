@@ -52,6 +52,7 @@ struct PagedAttnArgs {
   long parts_at, rows_at;  // floats before those of shares (the join's words), and before those of tiles of rows
   int shares;          // requests with a single row: shares of a key head's keys, 0: a workgroup for each request
   int single_waves;    // and its waves for each, 1, 2 or 4
+  int row_parts;       // parts of tiles of rows, of each key head, that the workspace holds
 };
 // A partial result: outputs of `cols` columns, then a maximum and a sum for each, in whole chunks of 16 bytes.
 __host__ __device__ inline size_t paged_part_floats(int cols, int hd) { return ((size_t)cols * (hd + 2) + 3) / 4 * 4; }

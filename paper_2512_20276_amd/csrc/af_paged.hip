@@ -257,7 +257,7 @@ bool paged_plan(int dtype, int head_dim, int n_kv_heads, int n_heads, int n_seq,
     // requests with a single row take n_seq rows at most; what is left may fill the GPU whatever the lengths are
     const long sure = (long)std::max(M - n_seq, 0) * group / row_tile * n_kv_heads;
     if (cap > split_keys && sure <= ROW_GRID / 2) {
-      p->row_split = 1;
+      p->row_split = true;
       join_rows = std::min(tiles * n_kv_heads * (row_tile / JOIN_COLS), (long)JOIN_GRID);
       // Tiles in two parts or more have fewer than twice as many as their keys are parts long: 2 ROW_GRID in all (and a little
       // for the sum's rounding).

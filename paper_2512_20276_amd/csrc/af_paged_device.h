@@ -268,6 +268,16 @@ __device__ __forceinline__ float wave_total(float x) {
   x = plus_dpp<0x143, 0xc>(plus_dpp<0x142, 0xa>(x));
   return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(x), 63));
 }
+// The largest of floats of 0 and more.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ float max_dpp(float x) {
+  return fmaxf(x, __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(x), CTRL, ROWS, 0xf, false)));
+}
+__device__ __forceinline__ float wave_max(float x) {
+  x = max_dpp<0x118, 0xf>(max_dpp<0x114, 0xf>(max_dpp<0x112, 0xf>(max_dpp<0x111, 0xf>(x))));
+  x = max_dpp<0x143, 0xc>(max_dpp<0x142, 0xa>(x));
+  return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(x), 63));
+}
 
 // ------------------------------------------------------------------ tiles of rows
 // The rows of a request with several, each with the heads that share a key head, are columns: column x is head x % group
@@ -310,10 +320,12 @@ struct RowTiles {
     per = 1 << 30;
     if (a.c.n_seq <= 64) read(a, 0);
     if constexpr (!SPLIT) return;
-    // What a workgroup would take if all tiles were split; then, of the requests that are split, what it takes if the
-    // tiles of the others have a workgroup each.  A split tile's parts are half a part more than its keys, on average.  Single
-    // rows beside them find an eighth of the places free (with none, four chunks and 28 single rows took 53 us instead of 43).
-    float share = 0.f;
+    // What a workgroup would take if all tiles were split; then, of the requests with longer tiles, what it takes if the
+    // tiles of the others have a workgroup each, and no less than the longest of those, so that it is these that stay whole
+    // and the parts are fewer than twice the places.  A split tile's parts are half a part more than its keys, on average.
+    // Single rows beside them find an eighth of the places free (with none, four chunks and 28 single rows took 53 us
+    // instead of 43).
+    float share = 0.f, longest = 0.f;  // of the tiles that are not split
 #pragma unroll 1
     for (int turn = 0; turn < 2; ++turn) {
       float work = 0.f, whole = 0.f;
@@ -321,7 +333,10 @@ struct RowTiles {
       for (int b0 = 0; b0 < a.c.n_seq; b0 += 64) {
         if (a.c.n_seq > 64) read(a, b0);
         float w = (float)n * (float)most, x = 0.5f * n;
-        if ((float)most <= share) w = 0.f, x = (float)n;
+        if ((float)most <= share) {
+          longest = fmaxf(longest, (float)most);
+          w = 0.f, x = (float)n;
+        }
         work += wave_total(w);
         whole += wave_total(x);
         singles |= __any(r.n == 1);
@@ -329,6 +344,7 @@ struct RowTiles {
       const float places = singles ? ROW_GRID * 7 / 8 : ROW_GRID;
       share = work * a.c.n_kv_heads / fmaxf(places - whole * a.c.n_kv_heads, ROW_GRID / 8);
     }
+    share = fmaxf(share, wave_max(longest));
     per = scalar(max((int)fminf(share, 1e9f) + 1, SPLIT_TILES<T>));  // (1e9: more than any tile has)
   }
   // Workgroup `at` of a key head: its tile and part.  JOIN: tile `at` of those that are split, part 0.
@@ -373,6 +389,8 @@ struct RowTiles {
     t.from = t.split * length;
     t.end = t.split == t.splits - 1 ? t.keys.n : t.from + length;
     if (t.split >= t.splits) t.b = -1;
+    // (starts that are not ascending give more parts than the workspace holds; no workgroup has taken those behind it)
+    if (JOIN && (t.part0 < 0 || t.part0 > a.row_parts - t.splits)) t.b = -1;
     return t;
   }
 };

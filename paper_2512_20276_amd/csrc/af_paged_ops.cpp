@@ -146,7 +146,7 @@ extern "C" af_status af_op_attention_paged(const af_paged_kv* kv, const void* q,
   a.scale_log2 = scale_log2;
   a.window = window ? window : INT_MAX, a.sinks = window ? n_sink : 0;
   a.parts = (float*)workspace, a.parts_at = p.parts_at, a.rows_at = p.rows_at;
-  a.shares = p.shares, a.single_waves = p.single_waves;
+  a.shares = p.shares, a.single_waves = p.single_waves, a.row_parts = p.row_grid / kv->n_kv_heads;
   AF_HIP(launch_attention_paged(kv->dtype, kv->head_dim, a, p, (hipStream_t)hip_stream));
   return AF_OK;
 }

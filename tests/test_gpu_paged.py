@@ -198,6 +198,32 @@ def test_many_requests_of_long_caches():
     check_attend(Step(requests, 1, 4, 64, 16, before=2, behind=5), window=700, sinks=9)
 
 
+@pytest.mark.parametrize("requests,Hkv,dtype", [([(2, 1100)] * 700, 1, BF16),
+                                                ([(2, 1100)] * 380 + [(9, 4000)] * 3 + [(1, 700)] * 4 + [(3, 40)] * 30, 1, BF16),
+                                                ([(3, 700), (1, 30)] * 60 + [(3, 5000)], 4, F32)])
+def test_many_requests_of_equal_long_caches(requests, Hkv, dtype):
+    """Tiles of rows that fill the GPU without a split, or nearly, beside longer ones."""
+    check_attend(Step(requests, Hkv, 1, 64, 64, dtype))
+
+
+def test_starts_that_are_not_ascending():
+    """No result means anything then, and nothing but the rows and the workspace is written."""
+    for n_seq, rows in ((200, 24), (40, 2), (900, 9)):
+        s = Step([(rows, 1200)] + [(0, 1200)] * 2, 1, 2, 64, 64)
+        s.to_gpu(af)
+        table = s.g["table"][:1].expand(n_seq, -1).contiguous()
+        lens = torch.full((n_seq,), 1200, dtype=torch.int32, device="cuda")
+        starts = torch.tensor([0, rows] * (n_seq // 2) + [0], dtype=torch.int32, device="cuda")
+        kv = af.PagedKV(s.g["k_cache"], s.g["v_cache"], table, lens, starts)
+        n = af.attention_paged_workspace(kv, rows, s.Hq)
+        around = torch.full((n + 8192,), 7, dtype=torch.uint8, device="cuda")
+        o = torch.full((rows + 20, s.Hq, s.hd), 7.0, dtype=BF16, device="cuda")
+        af.op_attention_paged(kv, s.g["q"], o[10:10 + rows], 0.125, around[4096:4096 + n])
+        torch.cuda.synchronize()
+        assert (around[:4096] == 7).all() and (around[4096 + n:] == 7).all()
+        assert (o[:10] == 7).all() and (o[10 + rows:] == 7).all()
+
+
 def test_the_same_inputs_give_the_same_bits():
     for requests, single in (([(1, 2000), (1, 5), (1, 900)], True), ([(30, 2000), (1, 1500), (9, 60)], False)):
         s = Step(requests, 2, 4, 128, 16, single=single)
