@@ -8,7 +8,12 @@ namespace af {
 // One workgroup a row.  Pair (j, j + HD/2) of a head turns by position * theta^(-2j/HD): in turns, and in 64 bits until
 // the whole turns are taken off, so that far positions keep their angle (an angle of 10^5 in 32 bits is off by
 // 0.004).  The row's HD/2 sines and cosines are computed once, by as many threads, while the row's queries, keys
-// and values are on their way, and read by all heads from LDS.  A thread rotates 8 pairs of a head at a time.
+// and values are on their way, and read by all heads from LDS.  A thread rotates 8 pairs of a head at a time, two chunks
+// of 16 bytes (fp32: four) whatever the type.
+// It moves bytes: 2264 rows of 32 + 32 + 32 bf16 heads of 128 (111 MB read and written) take 19.0 to 21.7 us, 5.1 to 5.8
+// TB/s; 282 such rows 5.3 us, of which 2.6 are the least that any launch here takes.  Loading the first heads ahead of
+// the sines made the large case slower (24.0 to 26.5 us a call): the waves in flight hide that already.
+
 // Eight elements whose address is a multiple of 16 bytes.
 template <typename T>
 struct Chunk8;
@@ -93,6 +98,8 @@ __global__ __launch_bounds__(256, 2) void attend_single_kernel(PagedAttnArgs a) 
 // ------------------------------------------------------------------ join
 // A head of a request with a single row, by a workgroup: groups of threads take parts of their own, with a running
 // maximum, and are joined in LDS.  The order of the sums goes by the parts' number alone.
+// What it reads comes from L2 or the cache behind it and is little: it is one chain of loads (the request and its word,
+// the parts' maxima and outputs, LDS, the store), 4.1 us for 48 requests of 32 heads, 5.1 for the 64 parts of one.
 template <typename T, int HD>
 __device__ __forceinline__ void join_single(const PagedAttnArgs& a, int b, int head) {
   constexpr int DT = HD / 4, GROUPS = 256 / DT;  // threads of a result, groups of threads
@@ -165,7 +172,10 @@ __device__ __forceinline__ void join_single(const PagedAttnArgs& a, int b, int h
 }
 
 // Tiles of rows that were split, JOIN_COLS columns at a time: a fixed number of workgroups that go on while there are
-// any, since only the lengths tell how many there are.
+// any, since only the lengths tell how many there are.  A thread has HD / 32 outputs of a column, so that a half wave
+// reads a part's column in one access, and eight parts are on their way at once.
+// Four chunks of 256 rows on about 6000 keys, beside 28 single rows: 8.2 us with the single rows' join, for 30 MB of
+// partial results that L2 holds in part.
 constexpr int JOIN_COLS = 8;
 constexpr int JOIN_GRID = 1024;
 template <typename T, int HD>
@@ -224,8 +234,14 @@ __global__ __launch_bounds__(256) void join_kernel(PagedAttnArgs a, int singles)
 }
 
 // ------------------------------------------------------------------ launch
-constexpr int SINGLE_GRID = 512;  // workgroups that the shares are to give: as many as the GPU holds at once
-constexpr int DIRECT_KEYS = 512;  // caches of so many keys at most are not split
+// Workgroups that the shares are to give: as many as the GPU holds at once (two a CU, 256 CUs).  48 requests of up to 16384
+// keys took 70.2 us with 512, more with 1024 and with 2048: the shares are equal, so more of them only add pieces, partial
+// results and beginnings.
+constexpr int SINGLE_GRID = 512;
+// Caches of so many keys at most are not split.  Unsplit against split, us a call: 64 requests of 283 keys, 32 key heads, 54.6
+// and 61.9; 8 of them 10.7 and 14.8; 64 of 512 keys, 8 key heads, 23.4 and 26.6, 8 of them 11.0 and 11.2.  At 1024 keys 8
+// requests take 18.3 and 14.1, one 14.3 and 9.7; 64 that are all of that length 49.5 and 52.9, but lengths differ.
+constexpr int DIRECT_KEYS = 512;
 bool paged_plan(int dtype, int head_dim, int n_kv_heads, int n_heads, int n_seq, bool single, int M, int cap, PagedPlan* p) {
   const int group = n_heads / n_kv_heads;
   const long head_blocks = (long)n_kv_heads * ((group + 15) / 16);
@@ -242,6 +258,9 @@ bool paged_plan(int dtype, int head_dim, int n_kv_heads, int n_heads, int n_seq,
     p->parts_at = ((long)n_seq * 2 + 3) / 4 * 4;
     floats = p->parts_at + shares * head_blocks * 2 * paged_part_floats(std::min(group, 16), head_dim);
   } else {
+    // Two or four requests' key heads in a workgroup once these alone fill the GPU twice or four times: a wave then works on
+    // alone, and where fewer would leave CUs without loads on their way, four share.  283 keys, 32 key heads: 64 requests on a
+    // wave each 54.6 us (four waves: 58.6), 32 on two 26.6 (30.4).  Of 100 keys, 128 on a wave each 47.3 (45.0).
     const long items = n_seq * head_blocks;
     p->single_waves = items >= 4 * SINGLE_GRID ? 1 : items >= 2 * SINGLE_GRID ? 2 : SINGLE_WAVES;
     const int each = SINGLE_WAVES / p->single_waves;
