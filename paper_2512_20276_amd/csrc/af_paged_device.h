@@ -323,8 +323,8 @@ struct RowTiles {
     // What a workgroup would take if all tiles were split; then, of the requests with longer tiles, what it takes if the
     // tiles of the others have a workgroup each, and no less than the longest of those, so that it is these that stay whole
     // and the parts are fewer than twice the places.  A split tile's parts are half a part more than its keys, on average.
-    // Single rows beside them find an eighth of the places free (with none, four chunks and 28 single rows took 53 us
-    // instead of 43).
+    // Single rows beside them find a quarter of the places free: four chunks and 28 single rows take 51 us a call, 53.5 with an
+    // eighth, more with none, 53 with three eighths and 73 with half.
     float share = 0.f, longest = 0.f;  // of the tiles that are not split
 #pragma unroll 1
     for (int turn = 0; turn < 2; ++turn) {
@@ -341,7 +341,7 @@ struct RowTiles {
         whole += wave_total(x);
         singles |= __any(r.n == 1);
       }
-      const float places = singles ? ROW_GRID * 7 / 8 : ROW_GRID;
+      const float places = singles ? ROW_GRID * 3 / 4 : ROW_GRID;
       share = work * a.c.n_kv_heads / fmaxf(places - whole * a.c.n_kv_heads, ROW_GRID / 8);
     }
     share = fmaxf(share, wave_max(longest));
@@ -398,6 +398,15 @@ template <typename T, bool SPLIT>
 __device__ __forceinline__ RowTile<ROW_KEYS<T>> row_tile(const PagedAttnArgs& a, int at) {
   RowTiles<T, SPLIT> tiles;
   tiles.init(a);
+  // Where all workgroups are on the GPU at once, two a CU, those that come second to a CU are taken in the opposite order: the
+  // longest tile then shares its CU with the shortest.  us, before and now: two prompts of 1024 rows, 32 heads on 8, 38.1 and
+  // 32.4, one of 2048 51.0 and 49.5, one of 1024 in fp32 171.8 and 145.5.
+  if (!SPLIT && a.c.n_seq <= 64) {
+    const int half = quotient(ROW_GRID / 2, a.n_kv_heads);
+    int n;
+    wave_prefix(tiles.n, n);
+    if (n * a.c.n_kv_heads <= ROW_GRID && at >= half && at < n) at = half + n - 1 - at;
+  }
   return tiles.template find<false>(a, at);
 }
 // Partial result of one part: cols x HD outputs, then a maximum and a sum for each column.

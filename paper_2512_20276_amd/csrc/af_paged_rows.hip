@@ -368,7 +368,7 @@ __device__ __forceinline__ void attend_tiles(const PagedAttnArgs& a, int block, 
 
 // fp32.  Four waves, 16 columns each, that read keys and values themselves: the matrix instructions of this
 // type, a sixteenth as fast, bound it, next the loads, which the four waves repeat from the vector cache (a prompt of 1024 rows,
-// 32 heads on 8: 177 us where its products alone are 56 at a large library product's 154 TFLOP/s).
+// 32 heads on 8: 145 us where its products alone are 56 at a large library product's 154 TFLOP/s).
 template <int HD, bool SPLIT>
 __device__ __forceinline__ void attend_rows(const PagedAttnArgs& a, int block) {
   typedef Columns<float, HD> C;

@@ -178,6 +178,12 @@ def test_one_request_of_a_packed_step(dtype):
     check_attend(Step([(0, 1900)], 2, 4, 64, 16, dtype, behind=2))
 
 
+@pytest.mark.parametrize("requests,dtype", [([(600, 600), (500, 700)], BF16), ([(300, 300), (1, 90), (260, 400)], F32)])
+def test_prompts_that_fill_the_gpu_once(requests, dtype):
+    """Tiles of rows for more than half of the workgroups that the GPU holds, and no more than all of them."""
+    check_attend(Step(requests, 4, 8, 64, 16, dtype, before=1, behind=2))
+
+
 def test_window_over_chunks_that_are_split():
     check_attend(Step([(20, 3000), (1, 2900)], 1, 4, 128, 16), window=1700, sinks=40)
 
