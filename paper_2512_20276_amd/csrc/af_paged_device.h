@@ -129,17 +129,14 @@ struct Columns {
 __device__ __forceinline__ bool not_finite(bf16 x) { return (__builtin_bit_cast(unsigned short, x) & 0x7f80) == 0x7f80; }
 __device__ __forceinline__ bool not_finite(float x) { return (__float_as_uint(x) & 0x7f800000u) == 0x7f800000u; }
 
-// One tile of keys j0 .. j0 + 31 of key head hk, whose pages the lanes hold (page_of).  p: the position of the lane's
-// column; lowest, highest: of all columns.  MANY: columns of several positions.
+// One tile of keys j0 .. j0 + 31 of key head hk, whose pages the lanes hold (page_of).  p: the position of all columns.
 // A lane loads 16 bytes of a key in each of KST steps, and its VJ values of eight keys: the keys 4 g .. 4 g + 3 of
-// either half of the tile, whose probabilities it holds.  Values that no column sees are replaced by zeros, since a
-// probability of 0 does not hide an infinity or a NaN; where only some columns see a value that is not finite the products
-// are taken one by one.
+// either half of the tile, whose probabilities it holds.  Values that are not seen are replaced by zeros, since a
+// probability of 0 does not hide an infinity or a NaN.
 // With bf16 values a probability is split into a bf16 head and a bf16 remainder, two products, so that it keeps
 // 16 bits: the cache's bytes bound these kernels, not the matrix instructions.
-template <typename T, int HD, bool MANY>
-__device__ __forceinline__ void attend_tile(const PagedAttnArgs& a, int hk, int j0, int page, int p, int lowest, int highest,
-                                            Columns<T, HD>& c) {
+template <typename T, int HD>
+__device__ __forceinline__ void attend_tile(const PagedAttnArgs& a, int hk, int j0, int page, int p, Columns<T, HD>& c) {
   typedef Columns<T, HD> C;
   typedef typename C::frag frag;
   constexpr int KST = C::KST, VJ = C::VJ;
@@ -175,22 +172,17 @@ __device__ __forceinline__ void attend_tile(const PagedAttnArgs& a, int hk, int 
 #pragma unroll
     for (int i = 0; i < 4; ++i) s[h * 4 + i] = acc[i] * a.scale_log2;
   }
-  const bool whole = all_see(a, lowest, highest, j0, KEY_TILE) && __all(page >= 0);
-  bool one_by_one = false;
+  const bool whole = all_see(a, p, p, j0, KEY_TILE) && __all(page >= 0);
   if (!whole) {
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
       const int j = j0 + (e >> 2) * 16 + lg * 4 + (e & 3);
-      const bool there = of_page[e >> 2] >= 0;
-      if (!there || !sees(a, p, j)) s[e] = -INFINITY;
-      const bool some = there && some_see(a, lowest, highest, j);
+      const bool seen = of_page[e >> 2] >= 0 && sees(a, p, j);
+      if (!seen) s[e] = -INFINITY;
 #pragma unroll
-      for (int d = 0; d < VJ; ++d) {
-        if (!some) v[e][d] = from_f<T>(0.f);
-        if (MANY) one_by_one |= not_finite(v[e][d]);
-      }
+      for (int d = 0; d < VJ; ++d)
+        if (!seen) v[e][d] = from_f<T>(0.f);
     }
-    if (MANY) one_by_one = __any(one_by_one);
   }
 
   float top = s[0];
@@ -215,31 +207,14 @@ __device__ __forceinline__ void attend_tile(const PagedAttnArgs& a, int hk, int 
     pf[e] = from_f<T>(s[e]);
     pl[e] = from_f<T>(s[e] - to_f(pf[e]));
   }
-  if (!MANY || !one_by_one) {
 #pragma unroll
-    for (int j = 0; j < VJ; ++j) {
-      frag vf;
+  for (int j = 0; j < VJ; ++j) {
+    frag vf;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) vf[e] = v[e][j];
-      c.o[j] = Mma<T>::mma(vf, pf, c.o[j]);
-      if constexpr (sizeof(T) == 2) c.o[j] = Mma<T>::mma(vf, pl, c.o[j]);
-    }
-    return;
+    for (int e = 0; e < 8; ++e) vf[e] = v[e][j];
+    c.o[j] = Mma<T>::mma(vf, pf, c.o[j]);
+    if constexpr (sizeof(T) == 2) c.o[j] = Mma<T>::mma(vf, pl, c.o[j]);
   }
-#pragma unroll
-  for (int e = 0; e < 8; ++e)
-#pragma unroll 1
-    for (int g = 0; g < 4; ++g) {
-      const int at = (e >> 2) * 16 + g * 4 + (e & 3), j = j0 + at;
-      const float w = __shfl(s[e], g * 16 + lr);
-      const int kp = __shfl(page, at);
-      if (kp < 0 || !sees(a, p, j)) continue;
-      const T* vrow = V + (kp * page_rows + head_row + (j & in_page)) * HD + lg * 4 * VJ;
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int d = 0; d < VJ; ++d) c.o[d][i] += w * to_f(vrow[i * VJ + d]);
-    }
 }
 
 // The natural logarithm of a column's sum of exponentials from its maximum and sum in powers of two.
@@ -515,7 +490,7 @@ __device__ __forceinline__ void attend_single(const PagedAttnArgs& a, int block,
       for (; i < i1; i += waves) {
         const int page = page_of_entry<KEY_TILE>(a.c, t.key(i), entry);
         if (i + waves < i1) entry = page_entry<KEY_TILE>(a.c, b, t.key(i + waves));
-        attend_tile<T, HD, false>(a, hk, t.key(i), page, p, p, p, c);
+        attend_tile<T, HD>(a, hk, t.key(i), page, p, c);
       }
       // ---- the waves' results, merged
       const float l = c.sum();

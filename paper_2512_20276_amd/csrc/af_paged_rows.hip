@@ -10,21 +10,58 @@ __device__ __forceinline__ float max_of_halves(float v) {  // of lane % 32 and l
   return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
 }
 
-// Tiles of 64 keys of a page pool in LDS, keys and values as they lie in the pages: rows of HD elements, the 16-byte
-// chunk c of row r at place c ^ turn(r) of the row.  With that the 16 rows of one access step of a key operand (the same
-// chunk of each) and the 8 rows x 64 bytes of a value operand are spread evenly over the banks.
-template <int HD>
+// Tiles of keys of a page pool in LDS, keys and values as they lie in the pages: rows of HD elements, the 16-byte chunk c of
+// row r at place c ^ turn(r) of the row.  With that the 16 rows of one access step of a key operand (the same chunk of each)
+// and, in bf16, the 8 rows x 64 bytes of a value operand are spread evenly over the banks.  (A value operand in fp32 is
+// neighbouring chunks of one row.)
+template <typename T, int HD>
 struct PageTiles {
-  static constexpr int KEYS = ROW_KEYS<bf16>, ROW = HD * 2, CHUNKS = HD / 8;
+  static constexpr int KEYS = ROW_KEYS<T>, ROW = HD * sizeof(T), CHUNKS = ROW / 16;
   static constexpr int BYTES = KEYS * ROW, STAGE = 2 * BYTES;
   static constexpr int STEP = 64 / CHUNKS;                // rows that a wave's load fills
-  static constexpr int LOADS = KEYS / STEP / 4;           // loads of a wave for a tile of keys, and of values
-  static_assert(8 % STEP == 0 && PAGED_MIN_PAGE >= 8 && LOADS * STEP == 16, "a load's rows lie in one page");
+  static constexpr int WAVE = KEYS / 4;                   // rows that a wave fills
+  static constexpr int LOADS = WAVE / STEP;               // with so many loads, of keys and of values
+  static_assert(8 % STEP == 0 && WAVE % 8 == 0 && PAGED_MIN_PAGE >= 8, "a load's rows lie in one page");
   __device__ __forceinline__ static int turn(int r) {
-    if constexpr (HD == 128) return (r & 3) << 2 | (r >> 2 & 3);
+    if constexpr (sizeof(T) == 4) return r & 15;
+    else if constexpr (HD == 128) return (r & 3) << 2 | (r >> 2 & 3);
     else return (r >> 1 & 1) << 2 | (r >> 2 & 3);
   }
+
+  unsigned lds, voff[LOADS];
+  int wave;
+  __device__ __forceinline__ void init(char* smem) {
+    const int lane = threadIdx.x & 63;
+    wave = scalar(threadIdx.x >> 6);
+    lds = scalar((unsigned)(uintptr_t)(__attribute__((address_space(3))) char*)smem);
+    // row `step row` + lane / CHUNKS of the tile, its chunk (lane % CHUNKS) ^ turn(row)
+#pragma unroll
+    for (int i = 0; i < LOADS; ++i) {
+      const int r = wave * WAVE + i * STEP + lane / CHUNKS;
+      voff[i] = (i * STEP % 8 + lane / CHUNKS) * ROW + (lane % CHUNKS ^ turn(r)) * 16;
+    }
+  }
+  // Sends for the tile of keys j0 .. of key head hk; pages: of key j0 + lane
+  __device__ __forceinline__ void load(const PagedAttnArgs& a, int hk, int j0, int pages, int buf) const {
+    const int in_page = (1 << a.c.page_shift) - 1;
+    // a wave's rows, in groups of 8 that lie in one page each
+#pragma unroll
+    for (int g = 0; g < WAVE / 8; ++g) {
+      const int r = wave * WAVE + g * 8;
+      const int page = max(__builtin_amdgcn_readlane(pages, r), 0);
+      const size_t at = ((((size_t)page * a.c.n_kv_heads + hk) << a.c.page_shift) + ((j0 + r) & in_page)) * ROW;
+      const unsigned dst = lds + buf * STAGE + r * ROW;
+#pragma unroll
+      for (int i = 0; i < 8 / STEP; ++i) {
+        const int n = g * (8 / STEP) + i;
+        dma16((const char*)a.c.k + at, voff[n], dst + i * STEP * ROW);
+        dma16((const char*)a.c.v + at, voff[n], dst + BYTES + i * STEP * ROW);
+      }
+    }
+  }
 };
+// This wave's loads are there, and every wave is done with what it read.
+__device__ __forceinline__ void loaded() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 
 // bf16.  Four waves of 32 columns each; the tiles of 64 keys go to LDS without passing registers, the next one while
 // this one is worked on.  Scores, and outputs, are taken transposed as in Columns: S^T = K . Q^T and O^T = V^T . P^T on
@@ -48,7 +85,7 @@ struct PageTiles {
 // order.
 template <int HD, bool SPLIT>
 __device__ __forceinline__ void attend_tiles(const PagedAttnArgs& a, int block, char* smem, int& odd_tile) {
-  typedef PageTiles<HD> L;
+  typedef PageTiles<bf16, HD> L;
   constexpr int TK = L::KEYS, COLS = ROW_TILE<bf16>, KST = HD / 16, OB = HD / 32;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), ln = lane & 31, h = lane >> 5;
   const int at = quotient(block, a.n_kv_heads), hk = remainder(block, a.n_kv_heads, at);
@@ -75,31 +112,9 @@ __device__ __forceinline__ void attend_tiles(const PagedAttnArgs& a, int block, 
     }
   }
 
-  // ---- loads: row `step row` + lane / CHUNKS of the tile, its chunk (lane % CHUNKS) ^ turn(row)
-  const unsigned lds0 = __builtin_amdgcn_readfirstlane((unsigned)(uintptr_t)(__attribute__((address_space(3))) char*)smem);
-  unsigned voff[L::LOADS];
-#pragma unroll
-  for (int i = 0; i < L::LOADS; ++i) {
-    const int r = (wave * L::LOADS + i) * L::STEP + lane / L::CHUNKS;
-    voff[i] = (i * L::STEP % 8 + lane / L::CHUNKS) * L::ROW + (lane % L::CHUNKS ^ L::turn(r)) * 16;
-  }
+  L tiles;
+  tiles.init(smem);
   const int in_page = (1 << a.c.page_shift) - 1;
-  const auto load = [&](int j0, int pages, int buf) {  // pages: of key j0 + lane
-    // a wave's 16 rows, in groups of 8 that lie in one page each
-#pragma unroll
-    for (int g = 0; g < 2; ++g) {
-      const int r = wave * 16 + g * 8;
-      const int page = max(__builtin_amdgcn_readlane(pages, r), 0);
-      const size_t at = ((((size_t)page * a.c.n_kv_heads + hk) << a.c.page_shift) + ((j0 + r) & in_page)) * L::ROW;
-      const unsigned dst = lds0 + buf * L::STAGE + r * L::ROW;
-#pragma unroll
-      for (int i = 0; i < 8 / L::STEP; ++i) {
-        const int n = g * (8 / L::STEP) + i;
-        dma16((const char*)a.c.k + at, voff[n], dst + i * L::STEP * L::ROW);
-        dma16((const char*)a.c.v + at, voff[n], dst + L::BYTES + i * L::STEP * L::ROW);
-      }
-    }
-  };
 
   // ---- LDS addresses: key ln of a block of 32, chunk 2 s + h; values 4 h + lane % 16 / 4 (and 8 further) of 16, dimensions
   // 16 (lane / 16 % 2) + 4 (lane % 4) of 32
@@ -126,7 +141,7 @@ __device__ __forceinline__ void attend_tiles(const PagedAttnArgs& a, int block, 
   int next = t.keys.key(i0);
   if (i0 < end) {
     pages = page_of<TK>(a.c, t.b, next);
-    load(next, pages, 0);
+    tiles.load(a, hk, next, pages, 0);
     if (i0 + 1 < end) entry = page_entry<TK>(a.c, t.b, t.keys.key(i0 + 1));
   }
   // Edge: some column does not see the whole tile
@@ -297,14 +312,13 @@ __device__ __forceinline__ void attend_tiles(const PagedAttnArgs& a, int block, 
   unsigned long long there = 0;
   const auto turn = [&]() {
     j0 = next;
-    // this tile is there, and every wave is done with the other one
-    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    loaded();  // this tile, and every wave is done with the other one
     there = __ballot(pages >= 0);
     here = pages;
     if (i + 1 < end) {
       next = t.keys.key(i + 1);
       pages = page_of_entry<TK>(a.c, next, entry);
-      load(next, pages, buf ^ 1);
+      tiles.load(a, hk, next, pages, buf ^ 1);
       if (i + 2 < end) entry = page_entry<TK>(a.c, t.b, t.keys.key(i + 2));
     }
     return j0 + TK <= full_end && (j0 >= full_from || j0 + TK <= a.sinks) && there == ~0ull;
@@ -366,49 +380,157 @@ __device__ __forceinline__ void attend_tiles(const PagedAttnArgs& a, int block, 
   }
 }
 
-// fp32.  Four waves, 16 columns each, that read keys and values themselves: the matrix instructions of this
-// type, a sixteenth as fast, bound it, next the loads, which the four waves repeat from the vector cache (a prompt of 1024 rows,
-// 32 heads on 8: 145 us where its products alone are 56 at a large library product's 154 TFLOP/s).
+// fp32.  Four waves of 16 columns each, tiles of 32 keys in LDS by turns as above, products transposed on 16 x 16 tiles as in
+// Columns.  A lane has keys 16 e + 4 g + 0..3 (g = lane / 16) of its column, and of a value's dimensions the chunks lane % 16
+// and, in heads of 128, 16 on; so its output of group j is element i of dimension 64 (j / 4) + 16 g + 4 i + j % 4.
+// The matrix instructions of this type, a sixteenth as fast as bf16's, bound it.
 template <int HD, bool SPLIT>
-__device__ __forceinline__ void attend_rows(const PagedAttnArgs& a, int block) {
+__device__ __forceinline__ void attend_rows(const PagedAttnArgs& a, int block, char* smem) {
   typedef Columns<float, HD> C;
-  constexpr int VJ = C::VJ, TK = KEY_TILE, COLS = ROW_TILE<float>;
-  static_assert(ROW_KEYS<float> == KEY_TILE && ROW_TILE<float> == 64, "four waves of 16 columns");
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, lr = lane & 15, lg = lane >> 4;
+  typedef PageTiles<float, HD> L;
+  constexpr int VJ = C::VJ, KST = C::KST, TK = L::KEYS, COLS = ROW_TILE<float>;
+  static_assert(TK == 32 && COLS == 64, "four waves of 16 columns");
+  const int lane = threadIdx.x & 63, wave = scalar(threadIdx.x >> 6), lr = lane & 15, lg = lane >> 4;
   const int at = quotient(block, a.n_kv_heads), hk = remainder(block, a.n_kv_heads, at);
   const RowTile<TK> t = row_tile<float, SPLIT>(a, at);
   if (t.b < 0) return;
   const int w0 = wave * 16;
-  if (w0 >= t.cols) return;
   const int col = t.col0 + min(w0 + lr, t.cols - 1);  // columns past the last one repeat it
   const int i_row = quotient(col, a.group), row = t.r.first + i_row, head = hk * a.group.d + remainder(col, a.group, i_row);
   const int base = t.r.len - t.r.n, p = base + i_row;
-  const int lowest = base + quotient(t.col0 + w0, a.group), highest = base + quotient(t.col0 + min(w0 + 15, t.cols - 1), a.group);
+  const int lowest = base + quotient(t.col0 + min(w0, t.cols - 1), a.group), highest = base + quotient(t.col0 + min(w0 + 15, t.cols - 1), a.group);
+  const int in_page = (1 << a.c.page_shift) - 1;
   C c;
   c.clear();
   c.load_q((const float*)a.q + row * a.q_stride + head * HD);
-  int entry = t.from < t.end ? page_entry<TK>(a.c, t.b, t.keys.key(t.from)) : -1;
-  for (int i = t.from; i < t.end; ++i) {
-    const int j0 = t.keys.key(i), page = page_of_entry<TK>(a.c, j0, entry);
-    if (i + 1 < t.end) entry = page_entry<TK>(a.c, t.b, t.keys.key(i + 1));
-    if (!none_see(a, lowest, highest, j0, TK)) attend_tile<float, HD, true>(a, hk, j0, page, p, lowest, highest, c);
+  L tiles;
+  tiles.init(smem);
+
+  const auto work = [&](int j0, int page, const char* tile) {
+    // ---- S^T = K . Q^T
+    f32x4 s2[2] = {f32x4{0.f, 0.f, 0.f, 0.f}, f32x4{0.f, 0.f, 0.f, 0.f}};
+#pragma unroll
+    for (int t = 0; t < KST; ++t) {
+      f32x4 kf[2][2];
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) kf[h][i] = *(const f32x4*)(tile + (h * 16 + lr) * L::ROW + ((t * 8 + lg * 2 + i) ^ L::turn(lr)) * 16);
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) s2[h] = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[h][e / 4][e % 4], c.q[t][e], s2[h], 0, 0, 0);
+    }
+    f32x4 v[8][VJ / 4];
+    int of_page[2];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const int r = (e >> 2) * 16 + lg * 4 + (e & 3);
+#pragma unroll
+      for (int d = 0; d < VJ / 4; ++d) v[e][d] = *(const f32x4*)(tile + L::BYTES + r * L::ROW + ((d * 16 + lr) ^ L::turn(r)) * 16);
+    }
+    float s[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) s[e] = s2[e >> 2][e & 3] * a.scale_log2;
+    // ---- masks: values that no column sees are replaced by zeros, since a probability of 0 does not hide an infinity or a NaN;
+    // where only some columns see a value that is not finite the products are taken one by one
+    bool one_by_one = false;
+    if (!(all_see(a, lowest, highest, j0, TK) && __all(page >= 0))) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h) of_page[h] = __shfl(page, h * 16 + lg * 4);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const int j = j0 + (e >> 2) * 16 + lg * 4 + (e & 3);
+        const bool there = of_page[e >> 2] >= 0;
+        if (!there || !sees(a, p, j)) s[e] = -INFINITY;
+        const bool some = there && some_see(a, lowest, highest, j);
+#pragma unroll
+        for (int d = 0; d < VJ; ++d) {
+          if (!some) v[e][d / 4][d % 4] = 0.f;
+          one_by_one |= not_finite(v[e][d / 4][d % 4]);
+        }
+      }
+      one_by_one = __any(one_by_one);
+    }
+    // ---- softmax
+    float top = s[0];
+#pragma unroll
+    for (int e = 1; e < 8; ++e) top = fmaxf(top, s[e]);
+    top = fmaxf(top, __shfl_xor(top, 16));
+    top = fmaxf(top, __shfl_xor(top, 32));
+    const float m = fmaxf(c.m, top), ref = m == -INFINITY ? 0.f : m;  // no key seen yet: probabilities and factor come out 0
+    if (__any(m > c.m)) {
+      const float f = __builtin_amdgcn_exp2f(c.m - ref);
+      c.l *= f;
+#pragma unroll
+      for (int j = 0; j < VJ; ++j) c.o[j] *= f;
+      c.m = m;
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      s[e] = __builtin_amdgcn_exp2f(s[e] - ref);
+      c.l += s[e];
+    }
+    // ---- O^T += V^T . P^T
+    if (!one_by_one) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+#pragma unroll
+        for (int j = 0; j < VJ; ++j) c.o[j] = __builtin_amdgcn_mfma_f32_16x16x4f32(v[e][j / 4][j % 4], s[e], c.o[j], 0, 0, 0);
+      return;
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+#pragma unroll 1
+      for (int g = 0; g < 4; ++g) {
+        const int r = (e >> 2) * 16 + g * 4 + (e & 3);
+        const float w = __shfl(s[e], g * 16 + lr);
+        const int kp = __builtin_amdgcn_readlane(page, r);
+        if (kp < 0 || !sees(a, p, j0 + r)) continue;
+        const float* vrow = (const float*)a.c.v + ((((size_t)kp * a.c.n_kv_heads + hk) << a.c.page_shift) + ((j0 + r) & in_page)) * HD + lg * 16;
+#pragma unroll
+        for (int j = 0; j < VJ; ++j)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) c.o[j][i] += w * vrow[j / 4 * 64 + i * 4 + j % 4];
+      }
+  };
+
+  int pages = -1, entry = -1;  // of this tile's keys; of the next one's, as the table has it
+  int next = t.keys.key(t.from);
+  if (t.from < t.end) {
+    pages = page_of<TK>(a.c, t.b, next);
+    tiles.load(a, hk, next, pages, 0);
+    if (t.from + 1 < t.end) entry = page_entry<TK>(a.c, t.b, t.keys.key(t.from + 1));
+  }
+  for (int i = t.from, buf = 0; i < t.end; ++i, buf ^= 1) {
+    const int j0 = next, page = pages;
+    loaded();  // this tile, and every wave is done with the other one
+    if (i + 1 < t.end) {
+      next = t.keys.key(i + 1);
+      pages = page_of_entry<TK>(a.c, next, entry);
+      tiles.load(a, hk, next, pages, buf ^ 1);
+      if (i + 2 < t.end) entry = page_entry<TK>(a.c, t.b, t.keys.key(i + 2));
+    }
+    if (w0 < t.cols && !none_see(a, lowest, highest, j0, TK)) work(j0, page, smem + buf * L::STAGE);
   }
   const float l = c.sum();
   if (w0 + lr >= t.cols) return;
   if (!SPLIT || t.splits == 1) {
     const float inv = l == 0.f ? 0.f : 1.0f / l;
-    float* dst = (float*)a.o + row * a.o_stride + head * HD + lg * 4 * VJ;
+    float* dst = (float*)a.o + row * a.o_stride + head * HD + lg * 16;
 #pragma unroll
-    for (int e = 0; e < 4; ++e)
+    for (int d = 0; d < VJ / 4; ++d)
 #pragma unroll
-      for (int j = 0; j < VJ; ++j) dst[e * VJ + j] = c.o[j][e] * inv;
+      for (int i = 0; i < 4; ++i)
+        *(f32x4*)(dst + d * 64 + i * 4) = f32x4{c.o[4 * d][i] * inv, c.o[4 * d + 1][i] * inv, c.o[4 * d + 2][i] * inv, c.o[4 * d + 3][i] * inv};
     if (a.lse && lg == 0) a.lse[(size_t)row * a.n_heads + head] = lse_of(c.m, l);
   } else {
     float* part = row_part(a, COLS, HD, t.part0 + t.split, hk);
 #pragma unroll
-    for (int e = 0; e < 4; ++e)
+    for (int d = 0; d < VJ / 4; ++d)
 #pragma unroll
-      for (int j = 0; j < VJ; ++j) part[(w0 + lr) * HD + (lg * 4 + e) * VJ + j] = c.o[j][e];
+      for (int i = 0; i < 4; ++i)
+        *(f32x4*)(part + (w0 + lr) * HD + d * 64 + lg * 16 + i * 4) = f32x4{c.o[4 * d][i], c.o[4 * d + 1][i], c.o[4 * d + 2][i], c.o[4 * d + 3][i]};
     if (lg == 0) {
       part[COLS * HD + 2 * (w0 + lr)] = c.m;
       part[COLS * HD + 2 * (w0 + lr) + 1] = l;
@@ -425,16 +547,15 @@ __global__ __launch_bounds__(256, 2) void attend_step_kernel(PagedAttnArgs a, in
   const int x = blockIdx.x;
   const bool single = x >= tiles && x < tiles + singles;
   const int block = single ? x - tiles : x < tiles ? x : x - singles;
-  if constexpr (sizeof(T) == 2) {
-    __shared__ __attribute__((aligned(1024))) char smem[2 * PageTiles<HD>::STAGE];
+  __shared__ __attribute__((aligned(1024))) char smem[2 * PageTiles<T, HD>::STAGE];
+  static_assert(sizeof(SingleLds<HD>) <= sizeof(smem), "one workgroup's LDS");
+  if (single) {
+    attend_single<T, HD>(a, block, *(SingleLds<HD>*)smem);
+  } else if constexpr (sizeof(T) == 2) {
     __shared__ int odd_tile;  // the last tile, counted from 1, that held values that are not finite
-    static_assert(sizeof(SingleLds<HD>) <= sizeof(smem), "one workgroup's LDS");
-    if (single) attend_single<T, HD>(a, block, *(SingleLds<HD>*)smem);
-    else attend_tiles<HD, SPLIT>(a, block, smem, odd_tile);
+    attend_tiles<HD, SPLIT>(a, block, smem, odd_tile);
   } else {
-    __shared__ __attribute__((aligned(16))) SingleLds<HD> lds;
-    if (single) attend_single<T, HD>(a, block, lds);
-    else attend_rows<HD, SPLIT>(a, block);
+    attend_rows<HD, SPLIT>(a, block, smem);
   }
 }
 
