@@ -375,7 +375,7 @@ __device__ __forceinline__ RowTile<ROW_KEYS<T>> row_tile(const PagedAttnArgs& a,
   tiles.init(a);
   // Where all workgroups are on the GPU at once, two a CU, those that come second to a CU are taken in the opposite order: the
   // longest tile then shares its CU with the shortest.  us, before and now: two prompts of 1024 rows, 32 heads on 8, 38.1 and
-  // 32.4, one of 2048 51.0 and 49.5, one of 1024 in fp32 171.8 and 145.5.
+  // 32.4, one of 2048 51.0 and 49.5, one of 1024 in fp32 (before its keys went through LDS) 171.8 and 145.5.
   if (!SPLIT && a.c.n_seq <= 64) {
     const int half = quotient(ROW_GRID / 2, a.n_kv_heads);
     int n;

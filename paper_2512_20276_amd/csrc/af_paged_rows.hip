@@ -30,9 +30,9 @@ struct PageTiles {
 
   unsigned lds, voff[LOADS];
   int wave;
-  __device__ __forceinline__ void init(char* smem) {
+  __device__ __forceinline__ void init(char* smem, int of_wave) {
     const int lane = threadIdx.x & 63;
-    wave = scalar(threadIdx.x >> 6);
+    wave = of_wave;
     lds = scalar((unsigned)(uintptr_t)(__attribute__((address_space(3))) char*)smem);
     // row `step row` + lane / CHUNKS of the tile, its chunk (lane % CHUNKS) ^ turn(row)
 #pragma unroll
@@ -113,7 +113,7 @@ __device__ __forceinline__ void attend_tiles(const PagedAttnArgs& a, int block, 
   }
 
   L tiles;
-  tiles.init(smem);
+  tiles.init(smem, wave);
   const int in_page = (1 << a.c.page_shift) - 1;
 
   // ---- LDS addresses: key ln of a block of 32, chunk 2 s + h; values 4 h + lane % 16 / 4 (and 8 further) of 16, dimensions
@@ -133,6 +133,7 @@ __device__ __forceinline__ void attend_tiles(const PagedAttnArgs& a, int block, 
     for (int e = 0; e < 16; ++e) o[c][e] = 0.f;
   float m = -INFINITY, l = 0.f;
 
+  const bool idle = w0 >= t.cols;  // a wave without a column only loads (16 chunks of 4 rows: 64 us instead of 67)
   // ---- the tiles: in LDS by turns, tile i + 1 on its way while tile i is worked on
   const int i0 = t.from, end = t.end;
   // tiles of keys in [full_from, full_end), or before full_sinks, are seen whole by all columns
@@ -175,7 +176,7 @@ __device__ __forceinline__ void attend_tiles(const PagedAttnArgs& a, int block, 
       if (odd) odd_tile = i + 1;
       __syncthreads();
       odd_values = odd_tile == i + 1;
-      if (none_see(a, lowest, highest, j0, TK)) return;
+      if (idle || none_see(a, lowest, highest, j0, TK)) return;
     }
     bf16x8 vf[2][OB];
     const auto read_v = [&](int k) {
@@ -332,7 +333,7 @@ __device__ __forceinline__ void attend_tiles(const PagedAttnArgs& a, int block, 
     bool whole = turn();
     if (whole) {
       do {
-        work(std::false_type{}, i, j0, there, here, buf);
+        if (!idle) work(std::false_type{}, i, j0, there, here, buf);
         done();
         if (i >= end) break;
         whole = turn();
@@ -383,7 +384,9 @@ __device__ __forceinline__ void attend_tiles(const PagedAttnArgs& a, int block, 
 // fp32.  Four waves of 16 columns each, tiles of 32 keys in LDS by turns as above, products transposed on 16 x 16 tiles as in
 // Columns.  A lane has keys 16 e + 4 g + 0..3 (g = lane / 16) of its column, and of a value's dimensions the chunks lane % 16
 // and, in heads of 128, 16 on; so its output of group j is element i of dimension 64 (j / 4) + 16 g + 4 i + j % 4.
-// The matrix instructions of this type, a sixteenth as fast as bf16's, bound it.
+// The matrix instructions of this type, a sixteenth as fast as bf16's, bound it: 3000 rows, 32 heads on 8 of 128, take 668 us, 110
+// TFLOP/s, 72 % of a large library product's 154; 1024 rows, where a CU has two workgroups in all, 102 us, 55 %.  With keys
+// and values from memory to each wave's registers, as single rows take them, these were 971 and 145.
 template <int HD, bool SPLIT>
 __device__ __forceinline__ void attend_rows(const PagedAttnArgs& a, int block, char* smem) {
   typedef Columns<float, HD> C;
@@ -404,7 +407,7 @@ __device__ __forceinline__ void attend_rows(const PagedAttnArgs& a, int block, c
   c.clear();
   c.load_q((const float*)a.q + row * a.q_stride + head * HD);
   L tiles;
-  tiles.init(smem);
+  tiles.init(smem, wave);
 
   const auto work = [&](int j0, int page, const char* tile) {
     // ---- S^T = K . Q^T
