@@ -280,6 +280,7 @@ struct RowTiles {
   Request r;
   int n, most;   // tiles of the lane's request, key tiles of its last one
   int per;       // key tiles of a part
+  int parts;     // of a tile of the lane's request
 
   __device__ __forceinline__ void read(const PagedAttnArgs& a, int b0) {
     const int b = b0 + (threadIdx.x & 63);
@@ -294,6 +295,7 @@ struct RowTiles {
   __device__ __forceinline__ void init(const PagedAttnArgs& a) {
     per = 1 << 30;
     if (a.c.n_seq <= 64) read(a, 0);
+    parts = 1;
     if constexpr (!SPLIT) return;
     // What a workgroup would take if all tiles were split; then, of the requests with longer tiles, what it takes if the
     // tiles of the others have a workgroup each, and no less than the longest of those, so that it is these that stay whole
@@ -321,6 +323,19 @@ struct RowTiles {
     }
     share = fmaxf(share, wave_max(longest));
     per = scalar(max((int)fminf(share, 1e9f) + 1, SPLIT_TILES<T>));  // (1e9: more than any tile has)
+    cut();
+  }
+  __device__ __forceinline__ void cut() { parts = SPLIT ? max((most + per - 1) / per, 1) : 1; }
+  // How many tiles are split.
+  __device__ __forceinline__ int split_tiles(const PagedAttnArgs& a) {
+    int some = 0;
+    for (int b0 = 0; b0 < a.c.n_seq; b0 += 64) {
+      if (a.c.n_seq > 64) read(a, b0), cut();
+      int all;
+      wave_prefix(parts > 1 ? n : 0, all);
+      some += all;
+    }
+    return some;
   }
   // Workgroup `at` of a key head: its tile and part.  JOIN: tile `at` of those that are split, part 0.
   template <bool JOIN>
@@ -329,8 +344,7 @@ struct RowTiles {
     t.b = -1;
     int before = 0, parts_before = 0, each = 1, length = per;
     for (int b0 = 0; b0 < a.c.n_seq; b0 += 64) {
-      if (a.c.n_seq > 64) read(a, b0);
-      const int parts = SPLIT ? max((most + per - 1) / per, 1) : 1;
+      if (a.c.n_seq > 64) read(a, b0), cut();
       const int weight = JOIN ? (parts > 1 ? n : 0) : n * parts;
       int all, all_parts = 0;
       const int prefix = wave_prefix(weight, all), of_parts = JOIN ? wave_prefix(n * parts, all_parts) : 0;
