@@ -77,7 +77,7 @@ __device__ __forceinline__ void loaded() { asm volatile("s_waitcnt vmcnt(0) lgkm
 // window's end, missing pages) mask scores, and clear values, in the tile's own place in LDS.
 // What bounds it: a wave's 32 matrix instructions of 32 clocks for a tile, and about 200 vector instructions (32 of them
 // exponentials), which the two waves of a SIMD run beside each other's matrix instructions.
-//   4096 rows, 32 heads on 8 key heads: 137 GFLOP in 147 us, 933 TFLOP/s, 73 % of a large library product's 1274; the
+//   4096 rows, 32 heads on 8 key heads: 137 GFLOP in 147 to 155 us, 933 to 888 TFLOP/s, 73 to 70 % of a large library product's 1274; the
 //   matrix cores are busy 52 % of the time at the clock that the power limit leaves.
 // Tried with no gain: a wave priority for its matrix instructions; a tile's scores one turn ahead of its exponentials;
 // half tiles by turns; loads spread between matrix instructions; tiles of 256 columns on eight waves (175 us against 163
