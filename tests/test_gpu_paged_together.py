@@ -134,6 +134,40 @@ def test_captured_and_replayed_with_other_lengths():
             assert torch.equal(o, want_o) and torch.equal(lse, want_lse), turn
 
 
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_captured_packed_rows_replayed_with_other_requests(dtype):
+    """A captured step of packed rows replays with other starts, so that prompts, chunks, single rows and requests without rows
+    change places, and with other lengths: keys that were split are not, and the other way round."""
+    for hkv, group, past in ((1, 4, 2500), (4, 8, 300)):
+        s = Step([(90, 100 + past)] * 4, hkv, group, 64, 16, dtype)
+        kv = s.to_gpu(af)
+        o = torch.zeros_like(s.g["q"])
+        ws = torch.empty(af.attention_paged_workspace(kv, s.M, s.Hq), dtype=torch.uint8, device="cuda")
+        step = lambda o: af.op_attention_paged(kv, s.g["q"], o, 0.1, ws)  # noqa: E731
+        step(o)
+        torch.cuda.synchronize()
+        graph, side = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+        with torch.cuda.graph(graph, stream=side):
+            step(o)
+        for counts in ([360, 0, 0, 0], [1, 1, 300, 1], [2, 355, 1, 2], [90, 90, 90, 90], [0, 0, 1, 4]):
+            lens = [max(n, (37 * i + 11 * n + past) % (100 + past)) for i, n in enumerate(counts)]
+            starts = [sum(counts[:i]) for i in range(5)]
+            kv.q_starts.copy_(torch.tensor(starts, dtype=torch.int32))
+            s.g["lens"].copy_(torch.tensor(lens, dtype=torch.int32))
+            o.fill_(7.0)
+            graph.replay()
+            torch.cuda.synchronize()
+            want = torch.full_like(o, 7.0)
+            step(want)
+            torch.cuda.synchronize()
+            assert torch.equal(o, want), counts
+            assert (o[starts[4]:] == 7).all()
+            scores = torch.full((s.M, s.Hq), -1.0, dtype=torch.float32, device="cuda")
+            af.op_attention_paged(kv, s.g["q"], want, 0.1, ws, 0, 0, scores)
+            rows = [starts[b] + i for b in range(4) for i in range(counts[b])]
+            assert torch.isfinite(scores[rows]).all()
+
+
 def test_several_streams():
     """Calls on streams of their own, with a workspace each, give what one behind the other gives."""
     steps = [Step([(9, 700), (1, 2000), (64, 64)], 2, 4, 128, 32, BF16, seed=i) for i in range(3)]
