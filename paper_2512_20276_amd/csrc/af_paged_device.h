@@ -129,6 +129,22 @@ struct Columns {
 __device__ __forceinline__ bool not_finite(bf16 x) { return (__builtin_bit_cast(unsigned short, x) & 0x7f80) == 0x7f80; }
 __device__ __forceinline__ bool not_finite(float x) { return (__float_as_uint(x) & 0x7f800000u) == 0x7f800000u; }
 
+// Two weights of 0 and more as bf16 heads and bf16 remainders, low half first.  A head is the weight cut to 8 bits, so that no
+// remainder is below 0, and the remainder is taken of the weight times 1 + 2^-23, so that it is above 0 where the weight is
+// (above 2^-100): a value that is infinite then gives that infinity in both products.  The two hold the weight to 2^-16.
+struct SplitPair {
+  unsigned head, rest;
+};
+__device__ __forceinline__ SplitPair split_pair(float a, float b) {
+  typedef __attribute__((__vector_size__(2 * sizeof(__bf16)))) __bf16 bf16x2;
+  const unsigned ua = __float_as_uint(a), ub = __float_as_uint(b);
+  constexpr float UP = 1.f + 0x1p-23f;
+  bf16x2 r;
+  r[0] = (bf16)__builtin_fmaf(a, UP, -__uint_as_float(ua & 0xffff0000u));
+  r[1] = (bf16)__builtin_fmaf(b, UP, -__uint_as_float(ub & 0xffff0000u));
+  return SplitPair{__builtin_amdgcn_perm(ub, ua, 0x07060302u), __builtin_bit_cast(unsigned, r)};
+}
+
 // One tile of keys j0 .. j0 + 31 of key head hk, whose pages the lanes hold (page_of).  p: the position of all columns.
 // A lane loads 16 bytes of a key in each of KST steps, and its VJ values of eight keys: the keys 4 g .. 4 g + 3 of
 // either half of the tile, whose probabilities it holds.  Values that are not seen are replaced by zeros, since a

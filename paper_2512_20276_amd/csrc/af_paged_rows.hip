@@ -70,19 +70,20 @@ __device__ __forceinline__ void loaded() { asm volatile("s_waitcnt vmcnt(0) lgkm
 // LDS reads that transpose 4 x 16 elements.
 // Outputs are scaled to a new maximum only when it passes the old one by 2^8 in some column: until then
 // probabilities go up to 2^8 instead of 1, with the same relative precision.
-// A probability is rounded to bf16 once (2^-8 of it at most): a remainder as in attend_tile would cost a third
-// more matrix instructions, which bound this kernel.  Sums are of the unrounded ones.
+// A probability is a bf16 head and a bf16 remainder (split_pair), as in attend_tile and in the ring's attention, so that a row is held
+// to the same 2^-16 whether it is alone in its request's step or not.  The remainder's products are half as many matrix
+// instructions again: 4096 rows took 156 us with one bf16 number (2^-8) and take 198.  Sums are of the unrounded ones.
 //
 // Tiles that every column sees whole have a loop of their own without any test of a key; tiles at an edge (the diagonal, a
 // window's end, missing pages) mask scores, and clear values, in the tile's own place in LDS.
-// What bounds it: a wave's 32 matrix instructions of 32 clocks for a tile, and about 200 vector instructions (32 of them
+// What bounds it: a wave's 48 matrix instructions of 32 clocks for a tile, and about 280 vector instructions (32 of them
 // exponentials), which the two waves of a SIMD run beside each other's matrix instructions.
-//   4096 rows, 32 heads on 8 key heads: 137 GFLOP in 147 to 155 us, 933 to 888 TFLOP/s, 73 to 70 % of a large library product's 1274; the
-//   matrix cores are busy 52 % of the time at the clock that the power limit leaves.
-// Tried with no gain: a wave priority for its matrix instructions; a tile's scores one turn ahead of its exponentials;
-// half tiles by turns; loads spread between matrix instructions; tiles of 256 columns on eight waves (175 us against 163
-// then); tiles of 32 keys with three waves a SIMD (the same here, short prompts slower); the longest tiles elsewhere in the
-// order.
+//   4096 rows, 32 heads on 8 key heads: 137 GFLOP in 198 us, 694 TFLOP/s, 54 % of a large library product's 1274; with the
+//   remainders' products 206 GFLOP, 1041 TFLOP/s.
+// Tried with no gain (before the remainders): a wave priority for its matrix instructions; a tile's scores one turn ahead of
+// its exponentials; half tiles by turns; loads spread between matrix instructions; tiles of 256 columns on eight waves (175 us
+// against 163); tiles of 32 keys with three waves a SIMD (the same here, short prompts slower); the longest tiles elsewhere in
+// the order.
 template <int HD, bool SPLIT>
 __device__ __forceinline__ void attend_tiles(const PagedAttnArgs& a, int block, char* smem, int& odd_tile) {
   typedef PageTiles<bf16, HD> L;
@@ -190,7 +191,7 @@ __device__ __forceinline__ void attend_tiles(const PagedAttnArgs& a, int block, 
       }
     };
     f32x16 s[2];
-    bf16x8 pf[4];
+    unsigned pf[4][4], pl[4][4];  // heads and remainders of the weights, operands of the second product
     {
       // ---- S^T = K . Q^T, four operands ahead
       bf16x8 kf[2][4];
@@ -271,10 +272,13 @@ __device__ __forceinline__ void attend_tiles(const PagedAttnArgs& a, int block, 
 #pragma unroll
       for (int b = 0; b < 2; ++b)
 #pragma unroll
-        for (int e = 0; e < 16; ++e) {
+        for (int e = 0; e < 16; e += 2) {
           s[b][e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][e], sl, -off));
-          sum[e & 1] += s[b][e];
-          pf[b * 2 + (e >> 3)][e & 7] = (bf16)s[b][e];
+          s[b][e + 1] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][e + 1], sl, -off));
+          sum[0] += s[b][e];
+          sum[1] += s[b][e + 1];
+          const SplitPair w = split_pair(s[b][e], s[b][e + 1]);
+          pf[b * 2 + (e >> 3)][e / 2 & 3] = w.head, pl[b * 2 + (e >> 3)][e / 2 & 3] = w.rest;
         }
       l += sum[0] + sum[1];
     }
@@ -283,12 +287,14 @@ __device__ __forceinline__ void attend_tiles(const PagedAttnArgs& a, int block, 
       constexpr int k = decltype(K)::value;
       if constexpr (k < 3) read_v(k + 1);
 #pragma unroll
-      for (int c = 0; c < OB; ++c) o[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[k & 1][c], pf[k], o[c], 0, 0, 0);
+      for (int c = 0; c < OB; ++c) o[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[k & 1][c], __builtin_bit_cast(bf16x8, pf[k]), o[c], 0, 0, 0);
+#pragma unroll
+      for (int c = 0; c < OB; ++c) o[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[k & 1][c], __builtin_bit_cast(bf16x8, pl[k]), o[c], 0, 0, 0);
       if constexpr (k < 3) {
 #pragma unroll
         for (int c = 0; c < OB; ++c) {
           __builtin_amdgcn_sched_group_barrier(0x100, 2, 1);
-          __builtin_amdgcn_sched_group_barrier(0x8, 1, 1);
+          __builtin_amdgcn_sched_group_barrier(0x8, 2, 1);
         }
       }
     });
