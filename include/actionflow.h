@@ -406,7 +406,8 @@ af_status af_attention_paged_workspace(const af_paged_kv* kv, int32_t M, int32_t
  *  workspace  of af_attention_paged_workspace bytes, aligned to 16; its contents before and after mean nothing.
  *       Calls that may run at the same time need one each (so do graphs that replay at the same time).
  * Scores, sums and outputs are held in fp32, and so is a weight that is multiplied with fp32 values; with bf16 values it is
- * two bf16 numbers, 2^-16 of it at most beside it, in every row.  A row's result may depend on the other rows through the order of
+ * two bf16 numbers, 2^-16 of it at most beside it, in every row.  A value that is infinite gives the rows that see it that
+ * infinity (with weights above 2^-100 of the row's largest; NaN beside one of the other sign).  A row's result may depend on the other rows through the order of
  * its sums, which goes by the lengths of all requests; it is the same for every run with the same sizes. */
 af_status af_op_attention_paged(const af_paged_kv* kv, const void* q, int64_t q_stride, void* o, int64_t o_stride,
                                 float* lse, int32_t M, int32_t n_heads, float scale, int32_t window, int32_t n_sink,

@@ -149,8 +149,8 @@ __device__ __forceinline__ SplitPair split_pair(float a, float b) {
 // A lane loads 16 bytes of a key in each of KST steps, and its VJ values of eight keys: the keys 4 g .. 4 g + 3 of
 // either half of the tile, whose probabilities it holds.  Values that are not seen are replaced by zeros, since a
 // probability of 0 does not hide an infinity or a NaN.
-// With bf16 values a probability is split into a bf16 head and a bf16 remainder, two products, so that it keeps
-// 16 bits: the cache's bytes bound these kernels, not the matrix instructions.
+// With bf16 values a probability is split into a bf16 head and a bf16 remainder (split_pair), two products, so that it keeps
+// 16 bits and infinite values stay what they are: the cache's bytes bound these kernels, not the matrix instructions.
 template <typename T, int HD>
 __device__ __forceinline__ void attend_tile(const PagedAttnArgs& a, int hk, int j0, int page, int p, Columns<T, HD>& c) {
   typedef Columns<T, HD> C;
@@ -220,8 +220,18 @@ __device__ __forceinline__ void attend_tile(const PagedAttnArgs& a, int hk, int 
   for (int e = 0; e < 8; ++e) {
     s[e] = __builtin_amdgcn_exp2f(s[e] - ref);
     c.l += s[e];
-    pf[e] = from_f<T>(s[e]);
-    pl[e] = from_f<T>(s[e] - to_f(pf[e]));
+  }
+  if constexpr (sizeof(T) == 2) {
+    unsigned head[4], rest[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const SplitPair w = split_pair(s[2 * e], s[2 * e + 1]);
+      head[e] = w.head, rest[e] = w.rest;
+    }
+    pf = __builtin_bit_cast(frag, head), pl = __builtin_bit_cast(frag, rest);
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) pf[e] = s[e];
   }
 #pragma unroll
   for (int j = 0; j < VJ; ++j) {

@@ -63,3 +63,27 @@ def test_a_row_is_as_exact_beside_another_as_alone():
     r, bound = held_to_16_bits(t, 0, 0)
     inside(attend(t), r, bound)
     inside(attend(s)[1:], r, bound)
+
+
+@pytest.mark.parametrize("dtype", [BF16, torch.float32])
+@pytest.mark.parametrize("hd,Hkv,group,page", [(128, 2, 4, 16), (64, 1, 17, 8)])
+@pytest.mark.parametrize("requests,single", [
+    ([(1, 41), (1, 64), (1, 1)], True),
+    ([(1, 700), (1, 64), (1, 2500)], True),  # split over the keys
+    ([(70, 100), (1, 64), (2, 130)], False),
+    ([(20, 700), (1, 2500), (3, 64)], False),  # split
+])
+def test_infinite_values_that_are_seen(dtype, hd, Hkv, group, page, requests, single):
+    """softmax . V gives the infinity to the rows that see it, NaN where both are seen, and to other dimensions what they had."""
+    for window in (0, 30):
+        s = Step(requests, Hkv, group, hd, page, dtype, single)
+        for b, (n, length) in enumerate(requests):
+            for j, d, worst in ((0, 0, math.inf), (length // 2, 5, -math.inf), (length - 1, 33, math.inf), (length - 1, 40, -math.inf),
+                                (max(length - 3, 0), 41, math.inf), (length - 1, 41, -math.inf)):
+                page_of, at = s.cell(b, j)
+                s.v_cache[page_of, :, at, d] = worst
+        got = attend(s, window)
+        want, bound, _, _ = s.attended(1.0 / math.sqrt(hd), window)
+        inside(got, want, bound, window)
+        mine = [row for row, _, _ in s.rows()]
+        assert torch.equal(got.cpu()[mine].isnan(), want[mine].isnan()), window
