@@ -366,7 +366,8 @@ af_status af_op_sample(int32_t dtype, const void* logits, int32_t n_rows, int32_
  *    outside [0, n_pages), or past the table, do not exist: they are not written, and nothing sees them.
  *    Requests may share pages that they only read.
  *  - AF_ERR_UNSUPPORTED: head_dim other than 64 and 128; a page_size that is no power of two or below 8; more
- *    than 2^30 keys in max_pages; M * n_heads of 2^30 or more; n_seq * max_pages * page_size / 32 past 2^31. */
+ *    than 2^30 keys in max_pages; M * n_heads of 2^30 or more; n_seq * (max_pages * page_size / 32 + 8) past
+ *    2^31 - 513. */
 typedef struct af_paged_kv {
   void* k;                   /* device [n_pages][n_kv_heads][page_size][head_dim] of dtype */
   void* v;                   /* likewise */

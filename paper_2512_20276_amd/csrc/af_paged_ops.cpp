@@ -36,7 +36,8 @@ af_status check_cache(const char* me, const af_paged_kv* kv, int32_t M, int32_t 
   const int64_t cap = (int64_t)kv->max_pages * kv->page_size;
   if (cap > PAGED_MAX_KEYS) return unsupported("a request's pages hold more than 2^30 keys");
   if ((int64_t)M * n_heads >= 1 << 30) return unsupported("M * n_heads is 2^30 or more");
-  if (kv->n_seq * (cap / 32 + 8) > INT_MAX) return unsupported("n_seq * max_pages * page_size / 32 is past 2^31");
+  // (single rows count tiles of 32 keys, up to three a request beside the table's, and the end of the last of 512 shares)
+  if (kv->n_seq * (cap / 32 + 8) > INT_MAX - 512) return unsupported("n_seq * max_pages * page_size / 32 is near 2^31 or past it");
   if (!aligned(kv->k, 16) || !aligned(kv->v, 16)) return unsupported("need 16-byte aligned k and v");
   *c = PagedCache{kv->k, kv->v, kv->page_table, kv->kv_lens, kv->q_starts, kv->n_pages, __builtin_ctz(kv->page_size),
                   kv->n_kv_heads, kv->n_seq, kv->max_pages, (int)cap, M};
