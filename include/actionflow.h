@@ -394,8 +394,9 @@ af_status af_op_rope_append_paged(const af_paged_kv* kv, const void* q, int64_t 
                                   const int32_t* sections, int32_t n_axes, float theta, void* q_out,
                                   int64_t q_out_stride, int32_t M, int32_t n_heads, void* hip_stream);
 
-/* Bytes of device workspace that af_op_attention_paged needs for these sizes (the cache's and its requests',
- * whether q_starts is there, M and n_heads; no pointer is followed).  It may be 0. */
+/* Bytes of device workspace that are enough for af_op_attention_paged at these sizes (the cache's and its requests',
+ * whether q_starts is there, M and n_heads; no pointer is followed), and with q_starts also for every step of fewer rows,
+ * requests or pages, without q_starts or with them: one asked for the largest step serves all.  It may be 0. */
 af_status af_attention_paged_workspace(const af_paged_kv* kv, int32_t M, int32_t n_heads, size_t* bytes);
 
 /* o = softmax(scale * q . k^T) v for M packed rows (rotated queries q [M][n_heads][head_dim], o likewise, rows

@@ -517,7 +517,8 @@ def op_rope_append_paged(kv: PagedKV, q: torch.Tensor, k: torch.Tensor, v: torch
 
 
 def attention_paged_workspace(kv: PagedKV, M: int, n_heads: int) -> int:
-    """Bytes of workspace that ``op_attention_paged`` needs for M rows of n_heads heads."""
+    """Bytes of workspace that are enough for ``op_attention_paged`` of M rows of n_heads heads, and where ``kv`` has q_starts
+    for every step of fewer rows, requests or pages too."""
     n = C.c_size_t()
     _check(lib.af_attention_paged_workspace(kv.ref, M, n_heads, C.byref(n)))
     return n.value

@@ -78,6 +78,8 @@ struct PagedPlan {
 };
 // False: more workgroups than a launch takes.
 bool paged_plan(int dtype, int head_dim, int n_kv_heads, int n_heads, int n_seq, bool single, int M, int cap, PagedPlan* p);
+// Floats of workspace that are enough for every step of up to M rows; false as above, for M rows.
+bool paged_workspace(int dtype, int head_dim, int n_kv_heads, int n_heads, int n_seq, bool single, int M, int cap, long* floats);
 hipError_t launch_attention_paged(int dtype, int head_dim, const PagedAttnArgs& a, const PagedPlan& p, hipStream_t s);
 hipError_t launch_paged_rows(int dtype, int head_dim, const PagedAttnArgs& a, const PagedPlan& p, hipStream_t s);
 

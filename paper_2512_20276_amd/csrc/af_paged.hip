@@ -248,6 +248,12 @@ constexpr int SINGLE_GRID = 512;
 // and 61.9; 8 of them 10.7 and 14.8; 64 of 512 keys, 8 key heads, 23.4 and 26.6, 8 of them 11.0 and 11.2.  At 1024 keys 8
 // requests take 18.3 and 14.1, one 14.3 and 9.7; 64 that are all of that length 49.5 and 52.9, but lengths differ.
 constexpr int DIRECT_KEYS = 512;
+// Rows beside one of each request, at most, of a step whose tiles may be split: so many tiles take half of the GPU's places.
+// (Requests with a single row take n_seq rows at most; what is left is in tiles whatever the lengths are.)
+static long split_rows(int row_tile, int n_kv_heads, int group) {
+  return ((ROW_GRID / 2 / n_kv_heads + 1L) * row_tile - 1) / group;
+}
+
 bool paged_plan(int dtype, int head_dim, int n_kv_heads, int n_heads, int n_seq, bool single, int M, int cap, PagedPlan* p) {
   const int group = n_heads / n_kv_heads;
   const long head_blocks = (long)n_kv_heads * ((group + 15) / 16);
@@ -279,9 +285,7 @@ bool paged_plan(int dtype, int head_dim, int n_kv_heads, int n_heads, int n_seq,
     const long columns = (long)M * group, tiles = columns / row_tile + std::min(n_seq, M / 2);  // at most so many
     row_grid = tiles * n_kv_heads;
     p->tile_grid = (int)std::min(row_grid, 1L << 24);
-    // requests with a single row take n_seq rows at most; what is left may fill the GPU whatever the lengths are
-    const long sure = (long)std::max(M - n_seq, 0) * group / row_tile * n_kv_heads;
-    if (cap > split_keys && sure <= ROW_GRID / 2) {
+    if (cap > split_keys && M - n_seq <= split_rows(row_tile, n_kv_heads, group)) {
       p->row_split = true;
       join_rows = std::min(tiles * n_kv_heads * (row_tile / JOIN_COLS), (long)JOIN_GRID);
       // Tiles in two parts or more have fewer than twice as many as their keys are parts long: 2 ROW_GRID in all (and a little
@@ -296,6 +300,20 @@ bool paged_plan(int dtype, int head_dim, int n_kv_heads, int n_heads, int n_seq,
   if (single_grid + row_grid >= most || join_singles + join_rows >= most) return false;
   p->single_grid = (int)single_grid, p->row_grid = (int)row_grid;
   p->join_singles = (int)join_singles, p->join_rows = (int)join_rows;
+  return true;
+}
+
+// The workspace grows with the rows up to where tiles are no longer split, and is smaller from there on; a single row of one
+// request is split where several are not.
+bool paged_workspace(int dtype, int head_dim, int n_kv_heads, int n_heads, int n_seq, bool single, int M, int cap, long* floats) {
+  PagedPlan p;
+  if (!paged_plan(dtype, head_dim, n_kv_heads, n_heads, n_seq, single, M, cap, &p)) return false;
+  *floats = p.floats;
+  if (single) return true;
+  const int row_tile = dtype == AF_BF16 ? ROW_TILE<bf16> : ROW_TILE<float>;
+  const long split = n_seq + split_rows(row_tile, n_kv_heads, n_heads / n_kv_heads);
+  for (const long rows : {1L, split})
+    if (rows < M && paged_plan(dtype, head_dim, n_kv_heads, n_heads, n_seq, single, (int)rows, cap, &p)) *floats = std::max(*floats, p.floats);
   return true;
 }
 

@@ -61,11 +61,7 @@ af_status check_rows(const char* me, const char* name, const af_paged_kv* kv, co
   return AF_OK;
 }
 
-af_status plan_of(const char* me, const af_paged_kv* kv, const PagedCache& c, int32_t n_heads, PagedPlan* p) {
-  if (!paged_plan(kv->dtype, kv->head_dim, c.n_kv_heads, n_heads, c.n_seq, !c.starts, c.M, c.cap, p))
-    return refuse(AF_ERR_UNSUPPORTED, me, "more workgroups than a launch takes");
-  return AF_OK;
-}
+af_status too_many(const char* me) { return refuse(AF_ERR_UNSUPPORTED, me, "more workgroups than a launch takes"); }
 
 }  // namespace
 
@@ -114,10 +110,10 @@ extern "C" af_status af_attention_paged_workspace(const af_paged_kv* kv, int32_t
   const char* me = "af_attention_paged_workspace";
   if (!bytes) return refuse(AF_ERR_INVALID_ARG, me, "bytes must be non-NULL");
   PagedCache c;
-  PagedPlan p;
+  long floats;
   AF_TRY(check_cache(me, kv, M, n_heads, &c));
-  AF_TRY(plan_of(me, kv, c, n_heads, &p));
-  *bytes = (size_t)p.floats * sizeof(float);
+  if (!paged_workspace(kv->dtype, kv->head_dim, c.n_kv_heads, n_heads, c.n_seq, !c.starts, M, c.cap, &floats)) return too_many(me);
+  *bytes = (size_t)floats * sizeof(float);
   return AF_OK;
 }
 
@@ -135,7 +131,7 @@ extern "C" af_status af_op_attention_paged(const af_paged_kv* kv, const void* q,
   const float scale_log2 = (float)(scale * 1.4426950408889634);
   if (!std::isfinite(scale_log2)) return refuse(AF_ERR_INVALID_ARG, me, "scale must be finite, and below 2^127");
   if (!aligned(lse, 4)) return refuse(AF_ERR_INVALID_ARG, me, "a pointer is not aligned to its element type");
-  AF_TRY(plan_of(me, kv, a.c, n_heads, &p));
+  if (!paged_plan(kv->dtype, kv->head_dim, kv->n_kv_heads, n_heads, kv->n_seq, !kv->q_starts, M, a.c.cap, &p)) return too_many(me);
   const size_t need = (size_t)p.floats * sizeof(float);
   if (need > 0 && (!workspace || workspace_bytes < need)) {
     set_error("%s: the workspace has %zu bytes, need %zu", me, workspace ? workspace_bytes : 0, need);
