@@ -14,18 +14,6 @@ namespace af {
 // TB/s; 282 such rows 5.3 us, of which 2.6 are the least that any launch here takes.  Loading the first heads ahead of
 // the sines made the large case slower (24.0 to 26.5 us a call): the waves in flight hide that already.
 
-// Eight elements whose address is a multiple of 16 bytes.
-template <typename T>
-struct Chunk8;
-template <>
-struct Chunk8<bf16> {
-  typedef bf16x8 type;
-};
-template <>
-struct Chunk8<float> {
-  typedef f32x8 type __attribute__((aligned(16)));
-};
-
 template <typename T, int HD>
 __global__ __launch_bounds__(256) void rope_append_kernel(AppendArgs a) {
   constexpr int HALF = HD / 2, PT = HALF / 8;  // threads of a head

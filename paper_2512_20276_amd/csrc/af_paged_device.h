@@ -15,6 +15,18 @@ __device__ __forceinline__ int scalar(int v) { return __builtin_amdgcn_readfirst
 __device__ __forceinline__ int quotient(int x, Divisor d) { return d.shift >= 0 ? x >> d.shift : x / d.d; }
 __device__ __forceinline__ int remainder(int x, Divisor d, int q) { return x - q * d.d; }
 
+// Eight elements whose address is a multiple of 16 bytes.
+template <typename T>
+struct Chunk8;
+template <>
+struct Chunk8<bf16> {
+  typedef bf16x8 type;
+};
+template <>
+struct Chunk8<float> {
+  typedef f32x8 type __attribute__((aligned(16)));
+};
+
 struct Request {
   int first, n, len;  // rows [first, first + n), cache length with them
 };
@@ -155,7 +167,7 @@ template <typename T, int HD>
 __device__ __forceinline__ void attend_tile(const PagedAttnArgs& a, int hk, int j0, int page, int p, Columns<T, HD>& c) {
   typedef Columns<T, HD> C;
   typedef typename C::frag frag;
-  constexpr int KST = C::KST, VJ = C::VJ;
+  constexpr int KST = C::KST, VJ = C::VJ, ALIGNED = VJ * sizeof(T) < 16 ? VJ * sizeof(T) : 16;  // pools are aligned to 16 bytes
   const int lane = threadIdx.x & 63, lr = lane & 15, lg = lane >> 4;
   const int in_page = (1 << a.c.page_shift) - 1;
   const size_t page_rows = (size_t)a.c.n_kv_heads << a.c.page_shift, head_row = (size_t)hk << a.c.page_shift;
@@ -169,14 +181,14 @@ __device__ __forceinline__ void attend_tile(const PagedAttnArgs& a, int hk, int 
     const int kp = max(__shfl(page, h * 16 + lr), 0);
     const T* krow = K + (kp * page_rows + head_row + ((j0 + h * 16 + lr) & in_page)) * HD + lg * 8;
 #pragma unroll
-    for (int s = 0; s < KST; ++s) kf[h][s] = *(const frag*)(krow + s * 32);
+    for (int s = 0; s < KST; ++s) kf[h][s] = *(const typename Chunk8<T>::type*)(krow + s * 32);
   }
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
     of_page[h] = __shfl(page, h * 16 + lg * 4);
     const T* vrow = V + (max(of_page[h], 0) * page_rows + head_row + ((j0 + h * 16 + lg * 4) & in_page)) * HD + lr * VJ;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) __builtin_memcpy(v[h * 4 + i], __builtin_assume_aligned(vrow + i * HD, VJ * sizeof(T)), VJ * sizeof(T));
+    for (int i = 0; i < 4; ++i) __builtin_memcpy(v[h * 4 + i], __builtin_assume_aligned(vrow + i * HD, ALIGNED), VJ * sizeof(T));
   }
 
   float s[8];
