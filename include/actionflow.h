@@ -387,8 +387,9 @@ typedef struct af_paged_kv {
  *  sections  host [n_axes]: how many pairs of a head turn with each axis, in order, head_dim / 2 in all (time,
  *            height and width of image patches, say); NULL for one axis.
  * Pair (j, j + head_dim / 2) turns by position * theta^(-2j / head_dim), as in the packed forward; the angle is
- * taken in 64 bits and each result rounded once.  Rows are independent; of two rows written to the same cell
- * (a page that two requests write) either may remain. */
+ * taken in 64 bits, its sine and cosine are rounded to fp32, and so are the products and their sum, which is rounded to the
+ * dtype once.  Rows are independent; of two rows written to the same cell (a page that two requests write) either may
+ * remain. */
 af_status af_op_rope_append_paged(const af_paged_kv* kv, const void* q, int64_t q_stride, const void* k,
                                   int64_t k_stride, const void* v, int64_t v_stride, const int32_t* positions,
                                   const int32_t* sections, int32_t n_axes, float theta, void* q_out,
@@ -409,8 +410,12 @@ af_status af_attention_paged_workspace(const af_paged_kv* kv, int32_t M, int32_t
  *       Calls that may run at the same time need one each (so do graphs that replay at the same time).
  * Scores, sums and outputs are held in fp32, and so is a weight that is multiplied with fp32 values; with bf16 values it is
  * two bf16 numbers, 2^-16 of it at most beside it, in every row.  A value that is infinite gives the rows that see it that
- * infinity (with weights above 2^-100 of the row's largest; NaN beside one of the other sign).  A row's result may depend on the other rows through the order of
- * its sums, which goes by the lengths of all requests; it is the same for every run with the same sizes. */
+ * infinity (with weights above 2^-100 of the row's largest; NaN beside one of the other sign).  A row's result may depend on
+ * the other rows through the order of its sums, which goes by the lengths of all requests; it is the same for every run with
+ * the same sizes.
+ * Long caches are split over the GPU.  Two steps' are not, and take the time of their longest cache on few CUs: those of a single
+ * request with M > 1 that turns out to have one row (a second request, without rows, has it split), and chunks beside about
+ * 32768 / n_heads rows (fp32: 16384 / n_heads) or more, prompts as a rule (a call of its own has them split). */
 af_status af_op_attention_paged(const af_paged_kv* kv, const void* q, int64_t q_stride, void* o, int64_t o_stride,
                                 float* lse, int32_t M, int32_t n_heads, float scale, int32_t window, int32_t n_sink,
                                 void* workspace, size_t workspace_bytes, void* hip_stream);

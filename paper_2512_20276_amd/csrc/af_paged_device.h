@@ -338,8 +338,8 @@ struct RowTiles {
     // What a workgroup would take if all tiles were split; then, of the requests with longer tiles, what it takes if the
     // tiles of the others have a workgroup each, and no less than the longest of those, so that it is these that stay whole
     // and the parts are fewer than twice the places.  A split tile's parts are half a part more than its keys, on average.
-    // Single rows beside them find a quarter of the places free: four chunks and 28 single rows take 51 us a call, 53.5 with an
-    // eighth, more with none, 53 with three eighths and 73 with half.
+    // Single rows beside them find a quarter of the places free: four chunks and 28 single rows take 58 us a call on a card that
+    // takes 60 with an eighth, 71 with none, 62.5 with three eighths and 87 with half.
     float share = 0.f, longest = 0.f;  // of the tiles that are not split
 #pragma unroll 1
     for (int turn = 0; turn < 2; ++turn) {
@@ -426,8 +426,8 @@ __device__ __forceinline__ RowTile<ROW_KEYS<T>> row_tile(const PagedAttnArgs& a,
   RowTiles<T, SPLIT> tiles;
   tiles.init(a);
   // Where all workgroups are on the GPU at once, two a CU, those that come second to a CU are taken in the opposite order: the
-  // longest tile then shares its CU with the shortest.  us, before and now: two prompts of 1024 rows, 32 heads on 8, 38.1 and
-  // 32.4, one of 2048 51.0 and 49.5, one of 1024 in fp32 (before its keys went through LDS) 171.8 and 145.5.
+  // longest tile then shares its CU with the shortest.  us, without that and with it: two prompts of 1024 rows, 32 heads on 8,
+  // 47.2 and 39, one of 2048 on 32 key heads 64 and 62, one of 1024 on 8 in fp32 118 and 100.5.
   if (!SPLIT && a.c.n_seq <= 64) {
     const int half = quotient(ROW_GRID / 2, a.n_kv_heads);
     int n;

@@ -76,10 +76,11 @@ __device__ __forceinline__ void loaded() { asm volatile("s_waitcnt vmcnt(0) lgkm
 //
 // Tiles that every column sees whole have a loop of their own without any test of a key; tiles at an edge (the diagonal, a
 // window's end, missing pages) mask scores, and clear values, in the tile's own place in LDS.
-// What bounds it: a wave's 48 matrix instructions of 32 clocks for a tile, and about 280 vector instructions (32 of them
+// What bounds it: a wave's 48 matrix instructions of 32 clocks for a tile, and about 330 vector instructions (32 of them
 // exponentials), which the two waves of a SIMD run beside each other's matrix instructions.
-//   4096 rows, 32 heads on 8 key heads: 137 GFLOP in 198 us, 694 TFLOP/s, 54 % of a large library product's 1274; with the
-//   remainders' products 206 GFLOP, 1041 TFLOP/s.
+//   4096 rows, 32 heads on 8 key heads: 137 GFLOP in 194 to 198 us, 708 to 694 TFLOP/s, 56 to 54 % of a large library product's
+//   1274; with the remainders' products 206 GFLOP.  The matrix cores are busy 63 % of the time at the clock that the power limit
+//   leaves.
 // Tried with no gain (before the remainders): a wave priority for its matrix instructions; a tile's scores one turn ahead of
 // its exponentials; half tiles by turns; loads spread between matrix instructions; tiles of 256 columns on eight waves (175 us
 // against 163); tiles of 32 keys with three waves a SIMD (the same here, short prompts slower); the longest tiles elsewhere in
@@ -548,8 +549,9 @@ __device__ __forceinline__ void attend_rows(const PagedAttnArgs& a, int block, c
 }
 
 // Tiles of rows and single rows in one launch, the tiles first: they take the longest, and single rows, which read memory
-// alone, fill the places that they leave.  (Alternating in eights, a prompt of 4096 rows without any single row took
-// 188 us instead of 159, four chunks with 28 single rows 56 instead of 45: the tiles began out of their order.)
+// alone, fill the places that they leave.  (Alternating in eights, before the weights' remainders, a prompt of 4096 rows without
+// any single row took 188 us instead of 159, four chunks with 28 single rows 56 instead of 45: the tiles began out of their
+// order.)
 // Workgroups of tiles beyond `tiles`, which are there if many keys are split, come last: most have nothing to do.
 template <typename T, int HD, bool SPLIT>
 __global__ __launch_bounds__(256, 2) void attend_step_kernel(PagedAttnArgs a, int tiles, int singles) {
